@@ -1,0 +1,405 @@
+"""Chunk attention over the paged cache, and a paged cache held in 8 bits: what their speed is measured on.
+
+Three paths of a serving loop over the pages of a shared pool:
+
+  chunk     several new tokens of every sequence at once: their keys and values are appended to the
+            sequence's pages and each token attends to the retained rows, the rows appended before, and
+            the chunk's tokens up to itself.  `kind` is what the pages hold: bf16, or 8 bits, where the
+            call quantises what it appends (the appended rows are read back too, as a loop that keeps a
+            copy of them does).  A chunk of one token is a decode step.
+  store     the retained rows of an evicted batch quantised into the pool's pages, and read back from
+            them as a contiguous bf16 cache.
+
+A row of 8-bit pages (one token, one KV head) is D codes and a power of two, 2^e: e is the least integer
+with max|x| <= M 2^e, and a code is x / 2^e rounded to nearest, ties to even, on the grid of its kind: fp8
+(e4m3, M = 448) or int8 (whole numbers, M = 127).
+"""
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+# Query heads, KV heads, head_dim of the shapes in workloads/configs.py and of the tests.
+_TINY = dict(hq=4, hkv=4, d=64)
+_MHA32 = dict(hq=32, hkv=32, d=128)
+_MHA40 = dict(hq=40, hkv=40, d=128)
+_GQA7 = dict(hq=28, hkv=4, d=128)
+_GQA4 = dict(hq=32, hkv=8, d=128)
+_GQA8_64 = dict(hq=16, hkv=2, d=64)
+
+_PLAIN = dict(chunk=1, ragged=False, reserve=128, page=16, kind="bf16", out="f32", gap=0.0)
+
+
+def _case(path, heads, batch, layers, tokens, rho, **more):
+    return dict(_PLAIN, path=path, batch=batch, layers=layers, tokens=tokens, rho=rho, **heads, **more)
+
+
+def listed():
+    cases = {
+        # one layer of a small model, two drafted tokens: a few workgroups, latency is all there is
+        "chunk_tiny": _case("chunk", _TINY, 1, 1, 168, 0.5, chunk=2, reserve=32),
+        # drafted tokens of a video batch checked in one call, each sequence with its own count; layers
+        # of very different budgets, one slot idle
+        "chunk_draft_video": _case("chunk", _GQA7, 8, 28, 8256, 0.05, chunk=5, ragged=True, gap=6.0),
+        # the next question about the same images, multi-head attention, all layers
+        "chunk_turn_llavanext": _case("chunk", _MHA32, 4, 32, 2979, 0.05, chunk=64, ragged=True, reserve=256),
+        # one layer of a 13B-class model takes the next question, as a forward pass calls it
+        "chunk_layer_13b": _case("chunk", _MHA40, 16, 1, 3171, 0.10, chunk=256, reserve=512, page=64),
+        # a further image joins the conversation: 1000 tokens on a pruned video cache, bf16 results
+        "chunk_image_video": _case("chunk", _GQA7, 4, 28, 8256, 0.05, chunk=1000, reserve=1280, page=64, out="bf16"),
+        # decode steps of the multi-tile batch and of the video batch on 8-bit pages
+        "decode_fp8_llavanext": _case("chunk", _MHA32, 4, 32, 2979, 0.05, kind="fp8"),
+        "decode_int8_video": _case("chunk", _GQA7, 8, 28, 8256, 0.10, kind="int8", gap=6.0),
+        # drafted tokens and the next question on 8-bit pages
+        "chunk_int8_draft_llava15": _case("chunk", _MHA32, 1, 32, 651, 0.10, chunk=4, kind="int8"),
+        "chunk_fp8_turn_video": _case("chunk", _GQA7, 8, 28, 8256, 0.05, chunk=48, ragged=True, kind="fp8", out="bf16"),
+        # one image question admitted into 8-bit pages; the multi-tile batch; a video batch at the larger share
+        "store_fp8_llava15": _case("store", _MHA32, 1, 32, 651, 0.10, kind="fp8"),
+        "store_int8_llavanext": _case("store", _MHA32, 4, 32, 2979, 0.10, kind="int8", gap=6.0),
+        "store_fp8_video": _case("store", _GQA7, 8, 28, 8256, 0.10, kind="fp8", page=64),
+    }
+    return [dict(c, name=n) for n, c in cases.items()]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    while True:
+        path = rng.choice(["chunk", "chunk", "chunk", "store"])
+        heads = rng.choice([_TINY, _MHA32, _MHA32, _MHA40, _GQA7, _GQA7, _GQA4, _GQA8_64])
+        chunk = 1 if path == "store" else rng.choice([1, _log(rng, 1, 16), _log(rng, 1, 1100), _log(rng, 8, 300)])
+        c = _case(path, heads, _log(rng, 1, 16), rng.choice([1, _log(rng, 1, 40), rng.randint(24, 40)]),
+                  _log(rng, 100, 9000), round(rng.uniform(0.03, 0.5), 3), chunk=chunk, ragged=rng.random() < 0.5,
+                  reserve=chunk + rng.choice([0, 1, 31, 64, 250]), page=rng.choice([1, 16, 16, 32, 64, 128]),
+                  kind=rng.choice(["fp8", "int8"] if path == "store" else ["bf16", "bf16", "fp8", "int8"]),
+                  out=rng.choice(["f32", "f32", "bf16"]), gap=rng.choice([0.0, 0.0, 6.0]))
+        if -(-(c["tokens"] + c["reserve"]) // c["page"]) > 4096:
+            continue
+        bl, rows = c["batch"] * c["layers"], min(c["tokens"], 4 * c["rho"] * c["tokens"]) + c["reserve"]
+        if bl * c["hq"] * chunk * rows * 4 > 20e9 or bl * c["hkv"] * rows * c["d"] * 4 > 8e9:
+            continue  # the plain form's logits and rows
+        if path == "store" and bl * c["hkv"] * c["tokens"] * c["d"] * 2 > 2e9:
+            continue
+        if work(c)["flops"] > 1.6e12 or work(c)["bytes"] > 1.2e9:
+            continue
+        return c
+
+
+# ------------------------------------------------------------------------------------- shapes
+def _total(c):
+    """Tokens that a sequence keeps over its layers."""
+    return max(1, int(math.floor(c["rho"] * c["tokens"] * c["layers"] + 0.5)))
+
+
+def _progress(c):
+    """Tokens appended before and new tokens of every sequence; (-1, 0) where a slot is idle."""
+    b = np.arange(c["batch"])
+    steps = (37 * b + 11) % (c["reserve"] - c["chunk"] + 1)
+    new = c["chunk"] - ((b * 5 + 1) % max(1, (c["chunk"] + 1) // 2) if c["ragged"] else 0 * b)
+    idle = (b % 8 == 5) & (c["path"] == "chunk")
+    return np.where(idle, -1, steps).astype(np.int32), np.where(idle, 0, new).astype(np.int32)
+
+
+def work(case):
+    c = case
+    row = c["hkv"] * c["d"]
+    held = 2 * row * 2 if c["kind"] == "bf16" else 2 * (row + c["hkv"])  # key and value of a token in the pages
+    if c["path"] == "store":
+        kept = c["batch"] * _total(c)
+        return {"bytes": kept * (2 * row * 2 + 4 + 2 * held + 2 * row * 2), "flops": 0}
+    steps, new = _progress(c)
+    steps, new = np.maximum(steps, 0).astype(np.int64), new.astype(np.int64)
+    live, layers = new > 0, c["layers"]
+    before = np.where(live, _total(c) + layers * steps, 0)  # rows over the layers
+    logits = (new * before + layers * new * (new + 1) // 2).sum()
+    n_new, n_before = int(new.sum()) * layers, int(before.sum())
+    moved = n_before * held + n_new * (2 * row * 2 + held)
+    moved += n_new * c["hq"] * c["d"] * (2 + (4 if c["out"] == "f32" else 2))
+    if c["kind"] != "bf16":
+        moved += n_new * (held + 2 * row * 2)
+    return {"bytes": moved, "flops": int(4 * c["d"] * c["hq"] * logits)}
+
+
+# ------------------------------------------------------------------------------------- inputs
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _randn(g, *shape, dtype=torch.bfloat16):
+    return torch.randn(*shape, generator=g, device="cuda", dtype=dtype)
+
+
+def _budgets(c, r):
+    """Layer budgets [B][L] in proportion to drawn masses, at most `tokens` each; every sequence's sum is
+    the same.  With `gap` shallow layers hold many times what middle layers do."""
+    out = []
+    for _ in range(c["batch"]):
+        x = np.arange(c["layers"]) / max(c["layers"] - 1, 1)
+        logit = -c["gap"] * (1.0 - 0.85 * np.exp(-x / 0.08) - 0.25 * x) + (0.5 if c["gap"] else 0.02) * r.standard_normal(c["layers"])
+        mass = 1.0 / (1.0 + np.exp(-logit)) + 0.01
+        b = np.minimum(np.floor(_total(c) * mass / mass.sum()).astype(np.int64), c["tokens"])
+        while b.sum() < _total(c):  # what rounding and full layers left over
+            open_ = np.nonzero(b < c["tokens"])[0]
+            more = -(-(_total(c) - int(b.sum())) // len(open_))
+            for i in open_:
+                b[i] += min(more, c["tokens"] - b[i], _total(c) - int(b.sum()))
+        out.append(b)
+    return np.stack(out).astype(np.int32)
+
+
+def _order(b):
+    """Longest segments first, as tgvkv_budget's unit_order."""
+    layers, batch = b.shape[1], b.shape[0]
+    o = np.empty((layers, batch), np.int32)
+    for i in range(batch):
+        o[:, i] = i * layers + np.argsort(-b[i].astype(np.int64), kind="stable")
+    return o.reshape(-1)
+
+
+def _table(c, b, r):
+    """The batch's pages, scattered over the pool: a table [B*L][max_pages] and the pool's size."""
+    need = -(-(b.reshape(-1).astype(np.int64) + c["reserve"]) // c["page"])
+    n_pages = (c["batch"] * (_total(c) + c["layers"] * (c["reserve"] + c["page"] - 1))) // c["page"]  # holds any split
+    ids, at = r.permutation(n_pages).astype(np.int32), 0
+    table = np.full((b.size, max(1, int(need.max()))), -1, np.int32)
+    for i, n in enumerate(need):
+        table[i, :n] = ids[at:at + n]
+        at += n
+    return table, n_pages
+
+
+def _inputs(c, seed):
+    """Everything of one case by name, tensors on the GPU."""
+    r, g = np.random.default_rng(int(seed)), _gen(seed)
+    b = _budgets(c, r)
+    table, n_pages = _table(c, b, r)
+    up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()  # noqa: E731
+    st = {"budgets": up(b), "table": up(table), "order": up(_order(b)), "longest": int(b.max())}
+    held = (n_pages, c["hkv"], c["page"], c["d"])
+    offsets = np.concatenate([[0], np.cumsum(b.reshape(-1).astype(np.int64))])
+    if c["path"] == "store":
+        st["k"], st["v"] = (_randn(g, c["batch"], c["layers"], c["hkv"], c["tokens"], c["d"]) for _ in range(2))
+        st["v"][..., 0] *= 4  # a channel that stands out
+        pick = [np.sort(r.choice(c["tokens"], n, replace=False)) for n in b.reshape(-1)]
+        st["idx"], st["idx_offsets"] = up(np.concatenate(pick).astype(np.int32)), up(offsets)
+        st["first"], st["count"], st["seg"], st["rows"] = None, st["budgets"].reshape(-1), st["idx_offsets"], int(offsets[-1])
+    else:
+        steps, new = _progress(c)
+        first = np.where(steps[:, None] < 0, 0, b + steps[:, None]).reshape(-1)
+        count = np.repeat(new, c["layers"])
+        seg = np.concatenate([[0], np.cumsum(count.astype(np.int64))])
+        st["steps"], st["new"], st["first"], st["count"], st["seg"] = up(steps), up(new), up(first.astype(np.int32)), up(count), up(seg)
+        st["rows"], st["longest"] = int(seg[-1]), int(first.max() + c["chunk"])
+        st["q"], st["k_new"], st["v_new"] = (_randn(g, c["batch"], c["layers"], c["chunk"], h, c["d"])
+                                             for h in (c["hq"], c["hkv"], c["hkv"]))
+        st["out"] = torch.zeros(c["batch"], c["layers"], c["chunk"], c["hq"], c["d"], device="cuda",
+                                dtype=torch.float32 if c["out"] == "f32" else torch.bfloat16)
+    for n in ("k", "v"):
+        if c["kind"] == "bf16":
+            st[n + "_pool"], st[n + "_exp"] = _randn(g, *held), None
+        elif c["path"] == "store":
+            st[n + "_pool"] = torch.zeros(held, dtype=torch.int8, device="cuda").view(_TYPE[c["kind"]])
+            st[n + "_exp"] = torch.zeros(held[:3], dtype=torch.uint8, device="cuda")
+        else:
+            st[n + "_pool"], st[n + "_exp"] = _quantise(_randn(g, *held), c["kind"])
+    if c["kind"] != "bf16":
+        st["k_rows"], st["v_rows"] = (torch.empty(st["rows"] * c["hkv"] * c["d"], dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    return st
+
+
+def prepare(case, seed):
+    return dict(_inputs(case, seed), case=dict(case))
+
+
+# ------------------------------------------------------------------------------------- a pass
+def run(state):
+    st, c = state, state["case"]
+    if own:
+        return _own_store(st) if c["path"] == "store" else _own_chunk(st)
+    return _plain_store(c, st) if c["path"] == "store" else _plain_chunk(c, st)
+
+
+def _handle(st):
+    """The pool, problem and workspace that a serving loop makes once and keeps."""
+    if "pool" not in st:
+        from paper_2606_03075_amd import binding as bd
+        c = st["case"]
+        kind = {"bf16": bd.CACHE_BF16, "fp8": bd.CACHE_FP8, "int8": bd.CACHE_INT8}[c["kind"]]
+        st["pool"] = bd.PagedPool(c["hkv"], c["d"], c["page"], 1, kind=kind)
+        st["pool"].attach(st["k_pool"], st["v_pool"], st["k_exp"], st["v_exp"])
+        st["problem"] = bd.make_problem(c["batch"], c["layers"], c["hq"], c["hkv"], c["d"], 0, c["tokens"], 0)
+        size = bd.chunk_workspace_size(st["problem"], None, c["chunk"])
+        st["ws"] = torch.empty(max(1, size), dtype=torch.uint8, device="cuda")
+    return st["pool"], st["problem"]
+
+
+def _own_chunk(st):
+    pool, problem = _handle(st)
+    pool.extend(problem, None, st["table"], st["budgets"], st["case"]["reserve"], st["steps"], st["new"], st["q"], st["k_new"],
+                st["v_new"], st["out"], st["ws"], unit_order=st["order"])
+    if st["k_exp"] is None:
+        return {"out": st["out"], "k_pool": st["k_pool"], "v_pool": st["v_pool"]}
+    pool.read(problem, None, st["table"], st["count"], st["seg"], st["k_rows"], st["v_rows"], first=st["first"])
+    return {"out": st["out"], "k_rows": st["k_rows"], "v_rows": st["v_rows"]}
+
+
+def _own_store(st):
+    pool, problem = _handle(st)
+    pool.store(problem, None, st["k"], st["v"], st["idx"], st["budgets"], st["idx_offsets"], _total(st["case"]), st["table"],
+               unit_order=st["order"])
+    pool.read(problem, None, st["table"], st["count"], st["seg"], st["k_rows"], st["v_rows"])
+    return {"k_rows": st["k_rows"], "v_rows": st["v_rows"]}
+
+
+# ------------------------------------------------------------------------------------- the plain form
+_TYPE = {"fp8": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def _quantise(x, kind):
+    """Codes and exponent bytes e + 127 of rows x [..., D]."""
+    f, k = torch.frexp(x.float().abs().amax(-1))  # max|x| = f 2^k, 0.5 <= f < 1
+    e = k - 9 + (f > 448 / 512) if kind == "fp8" else k - 7 + (f > 127 / 128)
+    e = torch.clamp(e, min=-100)
+    y = x.float() * torch.exp2(-e.float())[..., None]
+    codes = y.to(torch.float8_e4m3fn) if kind == "fp8" else torch.round(y).to(torch.int8)
+    return codes, (e + 127).to(torch.uint8)
+
+
+def _values(codes, exp):
+    return codes.float() * torch.exp2(exp.float() - 127)[..., None]
+
+
+def _rows_of(st):
+    """Segment and row within it of the `rows` rows that `count` and `seg` name, segment by segment."""
+    n = torch.arange(st["rows"], device="cuda")
+    bl = torch.searchsorted(st["seg"][1:].contiguous(), n, right=True)
+    return bl, n - st["seg"][bl]
+
+
+def _at(c, st, bl, row):
+    """Page and row in the page."""
+    return st["table"][bl, row // c["page"]].long(), row % c["page"]
+
+
+def _bytes(codes):
+    return codes.view(torch.int8) if codes.element_size() == 1 else codes
+
+
+def _write(c, st, name, page, row, x):
+    """x [rows, hkv, D] into a pool's pages."""
+    if c["kind"] == "bf16":
+        st[name + "_pool"][page, :, row] = x
+        return
+    codes, exp = _quantise(x, c["kind"])
+    _bytes(st[name + "_pool"])[page, :, row] = _bytes(codes)
+    st[name + "_exp"][page, :, row] = exp
+
+
+def _read(c, st, name, page, row):
+    """Rows [..., hkv, D] of a pool's pages, in 32 bits."""
+    codes = _bytes(st[name + "_pool"])[page, :, row]
+    return codes.float() if c["kind"] == "bf16" else _values(codes.view(_TYPE[c["kind"]]), st[name + "_exp"][page, :, row])
+
+
+def _read_back(c, st, bl, n, page, row):
+    """Rows of the pools as the segments [hkv][count][D] that `seg` names."""
+    head = torch.arange(c["hkv"], device="cuda")
+    to = st["seg"][bl][:, None] * c["hkv"] + head * st["count"][bl].long()[:, None] + n[:, None]
+    for name in ("k", "v"):
+        st[name + "_rows"].view(-1, c["d"])[to] = _read(c, st, name, page, row).to(torch.bfloat16)
+    return {"k_rows": st["k_rows"], "v_rows": st["v_rows"]}
+
+
+def _plain_store(c, st):
+    bl, n = _rows_of(st)
+    page, row = _at(c, st, bl, n)
+    for name in ("k", "v"):
+        _write(c, st, name, page, row, st[name].flatten(0, 1)[bl, :, st["idx"].long()])
+    return _read_back(c, st, bl, n, page, row)
+
+
+def _plain_chunk(c, st):
+    bl, n = _rows_of(st)
+    page, row = _at(c, st, bl, st["first"][bl] + n)
+    for name in ("k", "v"):
+        _write(c, st, name, page, row, st[name + "_new"].flatten(0, 1)[bl, n])
+    # every segment's rows, [B*L, hkv, longest, D]; what lies behind its last row counts nothing
+    pos = torch.arange(st["longest"], device="cuda")
+    all_bl = torch.arange(st["table"].shape[0], device="cuda")[:, None]
+    wide = torch.clamp(pos // c["page"], max=st["table"].shape[1] - 1)
+    pages = torch.clamp(st["table"][all_bl, wide], min=0).long()
+    k, v = (_read(c, st, name, pages, (pos % c["page"]).expand_as(pages)).transpose(1, 2) for name in ("k", "v"))
+    q = st["q"].flatten(0, 1).float().unflatten(2, (c["hkv"], -1)).transpose(1, 2).flatten(2, 3)  # [B*L, hkv, chunk * G, D]
+    z = torch.matmul(q, k.transpose(2, 3).contiguous()) * (1.0 / math.sqrt(c["d"]))
+    token = torch.arange(c["chunk"], device="cuda").repeat_interleave(c["hq"] // c["hkv"], output_size=q.shape[2])
+    z = z.masked_fill_((pos > st["first"][:, None, None] + token[:, None])[:, None], float("-inf"))
+    p = torch.exp(z.sub_(z.amax(-1, keepdim=True)))
+    o = torch.matmul(p, v) / p.sum(-1, keepdim=True)
+    o = o.unflatten(2, (c["chunk"], -1)).transpose(1, 2).flatten(2, 3)  # [B*L, chunk, hq, D]
+    live = torch.arange(c["chunk"], device="cuda") < st["count"][:, None]
+    out = st["out"].flatten(0, 1)
+    out.copy_(torch.where(live[:, :, None, None], o.to(out.dtype), out))
+    if c["kind"] == "bf16":
+        return {"out": st["out"], "k_pool": st["k_pool"], "v_pool": st["v_pool"]}
+    return dict(_read_back(c, st, bl, n, page, row), out=st["out"])
+
+
+# ------------------------------------------------------------------------------------- in 64 bits
+def _grid(x, kind):
+    """The values that rows x [..., D] stand for once held in 8 bits."""
+    x = x.double()
+    most = 448.0 if kind == "fp8" else 127.0
+    unit = torch.exp2(torch.ceil(torch.log2(x.abs().amax(-1, keepdim=True) / most)).clamp(min=-100))
+    y = x / unit
+    if kind == "int8":
+        return torch.round(y) * unit
+    step = torch.exp2(torch.floor(torch.log2(y.abs())).clamp(min=-6) - 3)  # e4m3: 3 bits, normal from 2^-6 on
+    return torch.round(y / step) * step * unit
+
+
+def exact(case, seed):
+    c = case
+    st = _inputs(c, seed)
+    b, table = st["budgets"].reshape(-1).tolist(), st["table"].tolist()
+    if c["path"] == "store":
+        got, at = {"k_rows": [], "v_rows": []}, 0
+        for i, n in enumerate(b):
+            for name in ("k", "v"):
+                x = st[name].flatten(0, 1)[i][:, st["idx"][at:at + n].long()]
+                got[name + "_rows"].append(_grid(x, c["kind"]).reshape(-1))
+            at += n
+        return {name: torch.cat(x) for name, x in got.items()}
+    held = (lambda x: x.double()) if c["kind"] == "bf16" else (lambda x: _grid(x, c["kind"]))
+    out = torch.zeros(st["out"].shape, dtype=torch.float64, device="cuda").flatten(0, 1)
+    first, count, group = st["first"].tolist(), st["count"].tolist(), c["hq"] // c["hkv"]
+    pools = [st[n].double() if st[e] is None else torch.ldexp(st[n].double(), st[e].double()[..., None] - 127)
+             for n, e in (("k_pool", "k_exp"), ("v_pool", "v_exp"))]
+    rows = [[], []]
+    for i in range(len(b)):
+        m = count[i]
+        if m == 0:
+            continue
+        ids = torch.tensor(table[i][:(first[i] + m - 1) // c["page"] + 1], device="cuda")
+        pos = torch.arange(first[i], first[i] + m, device="cuda")
+        kv = []
+        for pool, name, read in zip(pools, ("k_new", "v_new"), rows):
+            new = held(st[name].flatten(0, 1)[i, :m])  # [m, hkv, D]
+            pool[ids[pos // c["page"]], :, pos % c["page"]] = new
+            read.append(new.transpose(0, 1).reshape(-1))
+            kv.append(pool[ids].transpose(0, 1).flatten(1, 2)[:, :first[i] + m])
+        q = st["q"].flatten(0, 1)[i, :m].double().unflatten(1, (c["hkv"], group)).permute(1, 2, 0, 3)  # [hkv, G, m, D]
+        z = torch.matmul(q, kv[0][:, None].transpose(2, 3).contiguous()) / math.sqrt(c["d"])
+        hidden = torch.arange(first[i] + m, device="cuda") > pos[:, None]
+        p = torch.softmax(z.masked_fill_(hidden, float("-inf")), dim=-1)
+        out[i, :m] = torch.matmul(p, kv[1][:, None]).permute(2, 0, 1, 3).flatten(1, 2)
+    out = out.view(st["out"].shape)
+    if c["kind"] == "bf16":
+        return {"out": out, "k_pool": pools[0], "v_pool": pools[1]}
+    return {"out": out, "k_rows": torch.cat(rows[0]), "v_rows": torch.cat(rows[1])}
