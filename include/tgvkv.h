@@ -14,7 +14,9 @@
  *   tgvkv_decode_attn.
  * The same cache can instead live in fixed-size pages of a shared pool, for
  * serving with continuous batching: tgvkv_page_plan, tgvkv_page_table,
- * tgvkv_compact_paged, tgvkv_decode_attn_paged.
+ * tgvkv_compact_paged, tgvkv_decode_attn_paged; several new tokens per sequence
+ * in one call, and pages that hold 8 bits: tgvkv_compact_pages, tgvkv_read_pages,
+ * tgvkv_chunk_attn_pages.
  *
  * Conventions shared by every call
  *  - Token layout of each sequence: n_sys system-text tokens, then n_vis vision
@@ -365,6 +367,86 @@ tgvkv_status tgvkv_decode_attn_paged(const tgvkv_problem* problem, const tgvkv_o
                                      const int32_t* steps, const void* q, const void* k_new, const void* v_new,
                                      float* out, void* workspace, size_t workspace_bytes,
                                      const int32_t* unit_order_or_null, hipStream_t stream);
+
+/*
+ * Pages of any kind: several new tokens at once, and a cache in 8 bits.
+ *
+ * A pool described by tgvkv_pages is laid out as above, with `kind` what a row (one token, one KV head)
+ * is held as:
+ *   TGVKV_CACHE_BF16  head_dim bf16, as the paged calls above (the same pool serves both);
+ *   TGVKV_CACHE_FP8   head_dim e4m3 codes and one exponent byte;
+ *   TGVKV_CACHE_INT8  head_dim signed 8-bit codes and one exponent byte.
+ * The 8-bit kinds halve the cache and decode's reads.  A row x is held as
+ *   e = the least integer, at least -100, with max|x| <= M 2^e  (M = 448 for e4m3, 127 for whole numbers),
+ *   code = x / 2^e rounded to nearest, ties to even, on the kind's grid;  exponent byte e + 127,
+ * and stands for code * 2^e, which is exactly a bf16.  Per value the rounding is at most 2^-4 of it with
+ * e4m3 (at least 2^(e-10)), and 2^(e-1), so 1/127 of the row's largest, with whole numbers: INT8 is the finer
+ * kind for rows of even magnitude, FP8 for rows with a few large values.  A row that holds an infinity or
+ * a NaN gets codes 0 and the byte 255, and reads as NaN throughout.
+ */
+enum { TGVKV_CACHE_BF16 = 0, TGVKV_CACHE_FP8 = 1, TGVKV_CACHE_INT8 = 2 };
+
+typedef struct tgvkv_pages {
+    void*    k;          /* [n_pages][heads_kv][page_size][head_dim], bf16 or codes               */
+    void*    v;
+    uint8_t* k_exp;      /* [n_pages][heads_kv][page_size] exponent bytes; unused with BF16        */
+    uint8_t* v_exp;
+    int64_t  n_pages;    /* 1 .. 2^31 - 1                                                          */
+    int32_t  page_size;  /* a power of two in [1, 4096]                                            */
+    int32_t  kind;       /* TGVKV_CACHE_*                                                          */
+} tgvkv_pages;
+
+/* tgvkv_compact_pages -- tgvkv_compact_paged into pages of any kind: with an 8-bit kind every retained
+ * row is quantised as it is written, with BF16 it is that call.  Arguments and limits as there. */
+tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const void* k, const void* v,
+                                 const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
+                                 int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
+                                 int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream);
+
+/* tgvkv_read_pages -- rows of paged segments as contiguous bf16, the values that they stand for.
+ * For every (b, l), KV head h and n < count[b*L+l], row first[b*L+l] + n of the segment's pages goes to
+ *   k_out[(seg_offsets[b*L+l] * heads_kv + h * cap + n) * head_dim + :],  cap = seg_offsets[b*L+l+1] - seg_offsets[b*L+l],
+ * the segments' layout of tgvkv_compact.  Same for v.  With tgvkv_budget's seg_offsets and count = the rows
+ * held so far (budgets plus appended), k_out and v_out are a cache for tgvkv_decode_attn; with count = the new
+ * tokens of a chunk and first = the rows before them, they are what the chunk appended.
+ * first_or_null int32 [B*L] (null: 0);  count int32 [B*L], clamped to [0, cap];  seg_offsets int64 [B*L+1],
+ * ascending.  The rows read must be held: the table row covers them.  Slots count .. cap-1 are left as they
+ * are.  k_out, v_out bf16, seg_offsets[B*L] * heads_kv * head_dim elements each. */
+tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
+                              const int32_t* block_table, int32_t max_pages, const int32_t* first_or_null,
+                              const int32_t* count, const int64_t* seg_offsets, void* k_out, void* v_out,
+                              hipStream_t stream);
+
+/* tgvkv_chunk_attn_pages -- several new tokens of every sequence over the paged cache: drafted tokens to
+ * be checked, the next question, a further image; with chunk 1 a decode step, for pages of any kind.
+ *
+ * Sequence b, at step steps[b], brings c = n_new[b] tokens (chunk each with null).  For every layer, with
+ * f = budgets[b*L+l] + steps[b], it writes k_new / v_new of token i at row f + i of its pages, quantised
+ * with an 8-bit kind, and computes for each query head h
+ *   out[b][l][i][h] = softmax_n(tau q[b][l][i][h] . K[n]) V[n],  n <= f + i,
+ * over the rows as the pages hold them (Eq. (2)-(4); c decode steps in one call).
+ * A sequence takes no part, and its pages and rows of out are not touched, unless steps[b] >= 0,
+ * 1 <= c <= chunk and steps[b] + c <= decode_reserve; nor does a segment whose table row is too narrow
+ * for its f + c rows.  Tokens i >= c of the inputs are not read and their rows of out not touched.  A new
+ * row whose table entry is outside [0, n_pages) is not written.  Of `problem`, only batch, layers, heads and
+ * head_dim are used, as in tgvkv_decode_attn_paged.
+ *
+ * q            bf16 [B][L][chunk][heads_q][head_dim];  k_new, v_new bf16 [B][L][chunk][heads_kv][head_dim]
+ * steps, n_new_or_null  int32 [B], device
+ * out          [B][L][chunk][heads_q][head_dim], f32, or bf16 with out_bf16 != 0 (the probabilities then enter
+ *              the product with the values in bf16 too, which halves that product's work)
+ * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1 (TGVKV_E_UNSUPPORTED).
+ * workspace >= tgvkv_chunk_workspace_size(p, o, chunk) (may be 0 bytes), with any first contents; calls that
+ * may overlap need a workspace each.  unit_order_or_null as for tgvkv_decode_attn. */
+tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
+                                    const int32_t* block_table, int32_t max_pages, const int32_t* budgets,
+                                    int32_t decode_reserve, const int32_t* steps, const int32_t* n_new_or_null,
+                                    int32_t chunk, const void* q, const void* k_new, const void* v_new, void* out,
+                                    int32_t out_bf16, void* workspace, size_t workspace_bytes,
+                                    const int32_t* unit_order_or_null, hipStream_t stream);
+
+/* Workspace bytes of tgvkv_chunk_attn_pages for chunks of up to `chunk` tokens; 0 for an invalid problem or chunk. */
+size_t tgvkv_chunk_workspace_size(const tgvkv_problem* problem, const tgvkv_opts* opts, int32_t chunk);
 
 /* tgvkv_sizes -- host-only sizes that follow from the problem and options (no HIP call).
  * With the total_budget given to tgvkv_budget:

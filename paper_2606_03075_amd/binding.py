@@ -23,11 +23,13 @@ SCORE_STATS, SCORE_TEXT, SCORE_VISION, SCORE_ALL = 1, 2, 4, 7
 SCORE_LSE_IN = 16  # lse holds the text rows' normalisers from the caller's prefill: K is read once
 SCORE_ONE_ORDER = 32  # with any phases: every unit's keys summed in one run, not in shares
 CALL_SCORE, CALL_DECODE = 0, 1
+CACHE_BF16, CACHE_FP8, CACHE_INT8 = 0, 1, 2  # what the pages of a pool hold
 
 ABI_VERSION = 9  # TGVKV_ABI_VERSION of the library this binding marshals for
 EXPORTS = ("tgvkv_score", "tgvkv_budget", "tgvkv_select", "tgvkv_compact", "tgvkv_decode_attn",
            "tgvkv_decode_attn_noalloc",
            "tgvkv_page_plan", "tgvkv_page_table", "tgvkv_compact_paged", "tgvkv_decode_attn_paged",
+           "tgvkv_compact_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages", "tgvkv_chunk_workspace_size",
            "tgvkv_sizes", "tgvkv_workspace_size", "tgvkv_status_string", "tgvkv_abi_version")
 # measurement kernels (include/tgvkv_ceiling.h): the chip's achievable stream and matrix-core rates
 CEILING_EXPORTS = ("tgvkv_ceiling_read", "tgvkv_ceiling_copy", "tgvkv_ceiling_mfma", "tgvkv_ceiling_mfma_flops")
@@ -43,6 +45,12 @@ class TgvkvOpts(ctypes.Structure):
     _fields_ = [("sm_scale", ctypes.c_float), ("head_mode", ctypes.c_int32), ("n_sink", ctypes.c_int32),
                 ("n_recent", ctypes.c_int32), ("vision_only", ctypes.c_int32), ("budget_rule", ctypes.c_int32),
                 ("vision_rank", ctypes.c_int32), ("joint_rank", ctypes.c_int32)]
+
+
+class TgvkvPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kind", ctypes.c_int32)]
 
 
 class TgvkvError(RuntimeError):
@@ -63,6 +71,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     if not os.path.exists(p):
         raise RuntimeError(f"{p} is not built; run __graft_entry__.build() (hipcc for gfx950)")
     lib = ctypes.CDLL(p)
+    missing = [n for n in EXPORTS + CEILING_EXPORTS if not hasattr(lib, n)]
+    if missing:
+        raise RuntimeError(f"{p} has no {missing[0]}: it is older than this binding; rebuild it with "
+                           "__graft_entry__.build()")
     P = ctypes.POINTER(TgvkvProblem)
     O = ctypes.POINTER(TgvkvOpts)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -77,6 +89,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.tgvkv_compact_paged.argtypes = [P, O, vp, vp, vp, vp, vp, i64, vp, i32, i32, vp, vp, i64, vp, vp]
     lib.tgvkv_decode_attn_paged.argtypes = [P, O, vp, vp, i64, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz,
                                             vp, vp]
+    D = ctypes.POINTER(TgvkvPages)
+    lib.tgvkv_compact_pages.argtypes = [P, O, vp, vp, vp, vp, vp, i64, D, vp, i32, vp, vp]
+    lib.tgvkv_read_pages.argtypes = [P, O, D, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.tgvkv_chunk_attn_pages.argtypes = [P, O, D, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, i32, vp, sz, vp, vp]
+    lib.tgvkv_chunk_workspace_size.argtypes = [P, O, i32]
+    lib.tgvkv_chunk_workspace_size.restype = sz
     lib.tgvkv_sizes.argtypes = [P, O, i64, vp, vp]
     lib.tgvkv_workspace_size.argtypes = [P, O, i32]
     lib.tgvkv_workspace_size.restype = sz
@@ -90,6 +108,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.tgvkv_ceiling_mfma_flops.restype = ctypes.c_longlong
     for name in ("tgvkv_score", "tgvkv_budget", "tgvkv_select", "tgvkv_compact", "tgvkv_decode_attn",
                  "tgvkv_decode_attn_noalloc", "tgvkv_page_plan", "tgvkv_page_table", "tgvkv_compact_paged", "tgvkv_decode_attn_paged",
+                 "tgvkv_compact_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages",
                  "tgvkv_sizes", "tgvkv_abi_version", "tgvkv_ceiling_read", "tgvkv_ceiling_copy",
                  "tgvkv_ceiling_mfma"):
         getattr(lib, name).restype = ctypes.c_int32
@@ -148,6 +167,7 @@ def _check(fn: str, status: int):
 
 _torch = None  # torch, imported by the first call that is given a tensor
 _BF16, _F32, _I32, _I64 = "bf16", "f32", "i32", "i64"  # kinds of tensor arguments
+_OUT, _FP8, _INT8, _U8 = "f32 or bf16", "fp8", "int8", "u8"
 _KINDS = {}    # the element types of each kind
 
 
@@ -155,7 +175,8 @@ def _import_torch():
     global _torch
     import torch
     _KINDS.update({_BF16: (torch.bfloat16, torch.int16), _F32: (torch.float32,), _I32: (torch.int32,),
-                   _I64: (torch.int64,)})
+                   _I64: (torch.int64,), _OUT: (torch.float32, torch.bfloat16), _FP8: (torch.float8_e4m3fn,),
+                   _INT8: (torch.int8,), _U8: (torch.uint8,)})
     _torch = torch
 
 
@@ -369,6 +390,90 @@ def tgvkv_decode_attn_paged(problem, opts, k_pool, v_pool, page_size, block_tabl
     _check("tgvkv_decode_attn_paged", st)
 
 
+# --------------------------------------------------------------------------- pages of any kind
+def _pages(pool, problem):
+    """TgvkvPages of a PagedPool, after its tensors' checks against the problem."""
+    n = _pool_pages(pool.k_pool, pool.v_pool, problem, pool.page_size)
+    if pool.kind == CACHE_BF16:
+        return TgvkvPages(_ptr(pool.k_pool, _BF16, "k_pool"), _ptr(pool.v_pool, _BF16, "v_pool"), None, None, n,
+                          pool.page_size, pool.kind)
+    kind = _FP8 if pool.kind == CACHE_FP8 else _INT8
+    for name, t in (("k_exp", pool.k_exp), ("v_exp", pool.v_exp)):
+        if t is None or t.shape != pool.k_pool.shape[:3]:
+            raise ValueError(f"{name} must be [n_pages, heads_kv, page_size]")
+    return TgvkvPages(_ptr(pool.k_pool, kind, "k_pool"), _ptr(pool.v_pool, kind, "v_pool"),
+                      _ptr(pool.k_exp, _U8, "k_exp"), _ptr(pool.v_exp, _U8, "v_exp"), n, pool.page_size, pool.kind)
+
+
+def _sized(t, n, name):
+    """t, after checking that it holds n elements."""
+    if t is None or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements")
+    return t
+
+
+def chunk_workspace_size(problem, opts, chunk) -> int:
+    """Bytes of tgvkv_chunk_attn_pages' workspace for up to `chunk` new tokens per sequence."""
+    return int(load_library().tgvkv_chunk_workspace_size(ctypes.byref(problem), _opts_ref(opts), int(chunk)))
+
+
+def tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream=None,
+                        unit_order=None):
+    """tgvkv_compact_paged into a PagedPool of any kind (8-bit kinds: quantised as written)."""
+    st = load_library().tgvkv_compact_pages(ctypes.byref(problem), _opts_ref(opts), _ptr(k, _BF16, "k"),
+                                            _ptr(v, _BF16, "v"), _ptr(idx, _I32, "idx"),
+                                            _ptr(budgets, _I32, "budgets"), _ptr(idx_offsets, _I64, "idx_offsets"),
+                                            int(total_budget), ctypes.byref(_pages(pool, problem)),
+                                            _ptr(block_table, _I32, "block_table"), _table_width(block_table, problem),
+                                            _ptr(unit_order, _I32, "unit_order"), _stream(stream))
+    _check("tgvkv_compact_pages", st)
+
+
+def tgvkv_read_pages(problem, opts, pool, block_table, first, count, seg_offsets, k_out, v_out, stream=None):
+    """Rows of a PagedPool's segments, first (None: 0) .. first + count, as contiguous bf16 segments."""
+    n = problem.batch * problem.layers
+    if first is not None:
+        _sized(first, n, "first")
+    st = load_library().tgvkv_read_pages(ctypes.byref(problem), _opts_ref(opts), ctypes.byref(_pages(pool, problem)),
+                                         _ptr(block_table, _I32, "block_table"), _table_width(block_table, problem),
+                                         _ptr(first, _I32, "first"), _ptr(_sized(count, n, "count"), _I32, "count"),
+                                         _ptr(_sized(seg_offsets, n + 1, "seg_offsets"), _I64, "seg_offsets"),
+                                         _ptr(k_out, _BF16, "k_out"), _ptr(v_out, _BF16, "v_out"), _stream(stream))
+    _check("tgvkv_read_pages", st)
+
+
+def tgvkv_chunk_attn_pages(problem, opts, pool, block_table, budgets, decode_reserve, steps, n_new, q, k_new, v_new,
+                           out, workspace=None, stream=None, unit_order=None):
+    """Append up to chunk tokens per sequence and attend: q, out [B, L, chunk, heads_q, head_dim] (or [B, L,
+    heads_q, head_dim] for one token), k_new, v_new with heads_kv; n_new None: chunk tokens each.  out's type
+    (float32 or bfloat16) is the result's."""
+    p = problem
+    chunk = 1 if q.dim() == 4 else int(q.shape[2])
+    tokens = p.batch * p.layers * chunk * p.head_dim
+    _sized(q, tokens * p.heads_q, "q")
+    _sized(out, tokens * p.heads_q, "out")
+    _sized(k_new, tokens * p.heads_kv, "k_new")
+    _sized(v_new, tokens * p.heads_kv, "v_new")
+    _sized(budgets, p.batch * p.layers, "budgets")
+    _sized(steps, p.batch, "steps")
+    if n_new is not None:
+        _sized(n_new, p.batch, "n_new")
+    if unit_order is not None and unit_order.numel() < p.batch * p.layers:
+        raise ValueError("unit_order must hold batch * layers elements")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    st = load_library().tgvkv_chunk_attn_pages(ctypes.byref(problem), _opts_ref(opts),
+                                               ctypes.byref(_pages(pool, problem)),
+                                               _ptr(block_table, _I32, "block_table"),
+                                               _table_width(block_table, problem), _ptr(budgets, _I32, "budgets"),
+                                               int(decode_reserve), _ptr(steps, _I32, "steps"),
+                                               _ptr(n_new, _I32, "n_new"), chunk, _ptr(q, _BF16, "q"),
+                                               _ptr(k_new, _BF16, "k_new"), _ptr(v_new, _BF16, "v_new"),
+                                               _ptr(out, _OUT, "out"), int(out.dtype != _torch.float32),
+                                               _ptr(workspace, None, "workspace"), ws_bytes,
+                                               _ptr(unit_order, _I32, "unit_order"), _stream(stream))
+    _check("tgvkv_chunk_attn_pages", st)
+
+
 # --------------------------------------------------------------------------- whole-pass helpers
 class EvictionBuffers:
     """Device buffers of one eviction pass plus decode, allocated once for a problem.
@@ -487,19 +592,35 @@ class PagedPool:
     """A pool of cache pages shared by the sequences in service (continuous batching).
 
     Owns k_pool / v_pool [n_pages][heads_kv][page_size][head_dim] and the list of free
-    page ids.  admit() places a batch evicted into EvictionBuffers in the pool (page
-    table, then paged compaction); release() returns a finished sequence's pages.
-    Page assignment and every copy run in the library; this class only keeps the
-    free list, which needs the number of pages a batch took (one device read).
+    page ids; with an 8-bit kind (CACHE_FP8, CACHE_INT8) they hold codes, and k_exp / v_exp
+    [n_pages][heads_kv][page_size] the rows' exponent bytes.  admit() places a batch evicted into
+    EvictionBuffers in the pool (page table, then paged compaction); decode() takes a step, extend()
+    several new tokens per sequence, read() gives rows back as contiguous bf16; release() returns a
+    finished sequence's pages.  Page assignment and every copy run in the library; this class only keeps
+    the free list, which needs the number of pages a batch took (one device read).
     """
 
-    def __init__(self, heads_kv: int, head_dim: int, page_size: int, n_pages: int, device="cuda"):
+    def __init__(self, heads_kv: int, head_dim: int, page_size: int, n_pages: int, device="cuda",
+                 kind: int = CACHE_BF16):
         import torch
-        self.page_size, self.n_pages = int(page_size), int(n_pages)
-        self.k_pool = torch.empty((n_pages, heads_kv, page_size, head_dim), dtype=torch.bfloat16, device=device)
+        if kind not in (CACHE_BF16, CACHE_FP8, CACHE_INT8):
+            raise ValueError(f"unknown cache kind {kind!r}")
+        self.page_size, self.n_pages, self.kind = int(page_size), int(n_pages), int(kind)
+        dtype = (torch.bfloat16, torch.float8_e4m3fn, torch.int8)[self.kind]
+        self.k_pool = torch.empty((n_pages, heads_kv, page_size, head_dim), dtype=dtype, device=device)
         self.v_pool = torch.empty_like(self.k_pool)
+        self.k_exp = self.v_exp = None
+        if self.kind != CACHE_BF16:
+            self.k_exp = torch.empty((n_pages, heads_kv, page_size), dtype=torch.uint8, device=device)
+            self.v_exp = torch.empty_like(self.k_exp)
         self.free = list(range(n_pages))
         self.device = device
+
+    def attach(self, k_pool, v_pool, k_exp=None, v_exp=None):
+        """Serve from the caller's pool tensors (same page size and kind) instead of the pool's own."""
+        self.k_pool, self.v_pool, self.k_exp, self.v_exp = k_pool, v_pool, k_exp, v_exp
+        self.n_pages = int(k_pool.shape[0])
+        self.free = list(range(self.n_pages))
 
     def admit(self, buf: "EvictionBuffers", k, v, stream=None):
         """Page table [B*L, max_pages] of an evicted batch, with its rows compacted into the pool."""
@@ -513,11 +634,19 @@ class PagedPool:
         used = torch.zeros((1,), dtype=torch.int64, device=self.device)
         tgvkv_page_table(p, o, buf.budgets, buf.total_budget, buf.decode_reserve, self.page_size, ids, table, used,
                          stream)
-        tgvkv_compact_paged(p, o, k, v, buf.idx, buf.budgets, buf.idx_offsets, buf.total_budget, table,
-                            self.page_size, self.k_pool, self.v_pool, stream, buf.unit_order)
+        self.store(p, o, k, v, buf.idx, buf.budgets, buf.idx_offsets, buf.total_budget, table, stream, buf.unit_order)
         n = int(used.item()) if p.batch > 0 else 0
         del self.free[:n]
         return table
+
+    def store(self, problem, opts, k, v, idx, budgets, idx_offsets, total_budget, table, stream=None, unit_order=None):
+        """The retained rows of an evicted batch into the pages of its table, quantised with an 8-bit kind."""
+        if self.kind == CACHE_BF16:
+            tgvkv_compact_paged(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, table, self.page_size,
+                                self.k_pool, self.v_pool, stream, unit_order)
+        else:
+            tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, self, table, stream,
+                                unit_order)
 
     def release(self, table_rows):
         """Return the pages of finished sequences' table rows to the free list."""
@@ -526,7 +655,27 @@ class PagedPool:
 
     def decode(self, problem, opts, table, budgets, decode_reserve, steps, q, k_new, v_new, out, workspace,
                stream=None, unit_order=None):
-        """One decode step of a continuous batch whose sequence b is at step steps[b]."""
-        tgvkv_decode_attn_paged(problem, opts, self.k_pool, self.v_pool, self.page_size, table, budgets,
-                                decode_reserve, steps, q, k_new, v_new, out, workspace, stream, unit_order)
+        """One decode step of a continuous batch whose sequence b is at step steps[b].  workspace: CALL_DECODE's
+        with bf16 pages, chunk_workspace_size(problem, opts, 1) with an 8-bit kind."""
+        if self.kind == CACHE_BF16:
+            tgvkv_decode_attn_paged(problem, opts, self.k_pool, self.v_pool, self.page_size, table, budgets,
+                                    decode_reserve, steps, q, k_new, v_new, out, workspace, stream, unit_order)
+        else:
+            tgvkv_chunk_attn_pages(problem, opts, self, table, budgets, decode_reserve, steps, None, q, k_new, v_new,
+                                   out, workspace, stream, unit_order)
         return out
+
+    def extend(self, problem, opts, table, budgets, decode_reserve, steps, n_new, q, k_new, v_new, out, workspace,
+               stream=None, unit_order=None):
+        """Several new tokens per sequence: n_new[b] (None: all of the chunk) from step steps[b] on are appended
+        and attend to the sequence's rows and to one another, each up to itself.  q, out [B, L, chunk, heads_q,
+        head_dim], k_new, v_new [B, L, chunk, heads_kv, head_dim]; workspace: chunk_workspace_size bytes."""
+        tgvkv_chunk_attn_pages(problem, opts, self, table, budgets, decode_reserve, steps, n_new, q, k_new, v_new, out,
+                               workspace, stream, unit_order)
+        return out
+
+    def read(self, problem, opts, table, count, seg_offsets, k_out, v_out, first=None, stream=None):
+        """Rows first .. first + count of every segment as contiguous bf16 [heads_kv][capacity][head_dim] segments
+        at seg_offsets (tgvkv_compact's layout)."""
+        tgvkv_read_pages(problem, opts, self, table, first, count, seg_offsets, k_out, v_out, stream)
+        return k_out, v_out

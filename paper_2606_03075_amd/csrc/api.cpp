@@ -171,7 +171,31 @@ void page_plan(const Shape& s, int64_t total_budget, int32_t reserve, int32_t pa
             page_size;
 }
 
+// A pool's description and table width as the kernels take them, after its checks.
+tgvkv_status make_pages(const tgvkv_pages* d, int32_t max_pages, const int32_t* block_table, tgvkv::Pages* pg) {
+    if (d == nullptr) return TGVKV_E_INVAL;
+    const int32_t sh = page_shift(d->page_size);
+    if (sh < 0 || max_pages < 1 || d->n_pages < 1) return TGVKV_E_INVAL;
+    if (d->kind != TGVKV_CACHE_BF16 && d->kind != TGVKV_CACHE_FP8 && d->kind != TGVKV_CACHE_INT8) return TGVKV_E_INVAL;
+    if (max_pages > kMaxTablePages || d->n_pages > INT32_MAX) return TGVKV_E_UNSUPPORTED;
+    *pg = tgvkv::Pages{static_cast<uint8_t*>(d->k), static_cast<uint8_t*>(d->v), d->k_exp, d->v_exp,
+                       static_cast<int32_t>(d->n_pages), sh, d->kind, block_table, max_pages};
+    return TGVKV_OK;
+}
+
+// Chunks whose query rows the kernels can number in 32 bits.
+bool chunk_fits(const Shape& s, int32_t chunk) {
+    return chunk >= 1 && (int64_t)s.B * s.L * s.H <= kMaxBlocks / chunk;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The pool's and the table's memory, needed by every call that has work to do.
+bool pages_present(const tgvkv::Pages& pg) {
+    if (pg.k == nullptr || pg.v == nullptr || pg.table == nullptr || !aligned16(pg.k) || !aligned16(pg.v)) return false;
+    return pg.kind == TGVKV_CACHE_BF16 ||
+           (pg.k_exp != nullptr && pg.v_exp != nullptr && aligned16(pg.k_exp) && aligned16(pg.v_exp));
+}
 
 tgvkv_status hip_status(hipError_t e) { return e == hipSuccess ? TGVKV_OK : TGVKV_E_HIP; }
 
@@ -477,4 +501,85 @@ tgvkv_status tgvkv_decode_attn_paged(const tgvkv_problem* problem, const tgvkv_o
         static_cast<const uint16_t*>(v_new), out, static_cast<float*>(workspace), unit_order_or_null, stream));
 }
 
-}  // extern "C\"
+tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const void* k, const void* v,
+                                 const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
+                                 int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
+                                 int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream) {
+    Shape s;
+    tgvkv_status st = make_shape(problem, opts, &s);
+    if (st != TGVKV_OK) return st;
+    tgvkv::Pages pg;
+    st = make_pages(pages, max_pages, block_table, &pg);
+    if (st != TGVKV_OK) return st;
+    if (pg.kind == TGVKV_CACHE_BF16)
+        return tgvkv_compact_paged(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, block_table, max_pages,
+                                   pages->page_size, pages->k, pages->v, pages->n_pages, unit_order_or_null, stream);
+    if (total_budget < 0) return TGVKV_E_INVAL;
+    if (total_budget > budget_capacity(s)) return TGVKV_E_CAPACITY;
+    if ((max_layer_budget(s, total_budget) + pages->page_size - 1) / pages->page_size > max_pages)
+        return TGVKV_E_CAPACITY;
+    const int64_t kept = kept_per_sequence(s, total_budget);
+    if (s.B == 0 || kept == 0) return TGVKV_OK;
+    if (k == nullptr || v == nullptr || idx == nullptr || budgets == nullptr || idx_offsets == nullptr ||
+        !pages_present(pg))
+        return TGVKV_E_INVAL;
+    if (!aligned16(k) || !aligned16(v)) return TGVKV_E_INVAL;
+    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    return hip_status(tgvkv::launch_compact_pages(s, pg, static_cast<const uint16_t*>(k),
+                                                  static_cast<const uint16_t*>(v), idx, budgets, idx_offsets,
+                                                  (int64_t)s.B * kept, unit_order_or_null, stream));
+}
+
+tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
+                              const int32_t* block_table, int32_t max_pages, const int32_t* first_or_null,
+                              const int32_t* count, const int64_t* seg_offsets, void* k_out, void* v_out,
+                              hipStream_t stream) {
+    Shape s;
+    tgvkv_status st = make_shape(problem, opts, &s);
+    if (st != TGVKV_OK) return st;
+    tgvkv::Pages pg;
+    st = make_pages(pages, max_pages, block_table, &pg);
+    if (st != TGVKV_OK) return st;
+    if (s.B == 0) return TGVKV_OK;
+    if (!pages_present(pg) || count == nullptr || seg_offsets == nullptr || k_out == nullptr || v_out == nullptr)
+        return TGVKV_E_INVAL;
+    if (!aligned16(k_out) || !aligned16(v_out)) return TGVKV_E_INVAL;
+    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    return hip_status(tgvkv::launch_read_pages(s, pg, first_or_null, count, seg_offsets, static_cast<uint16_t*>(k_out),
+                                               static_cast<uint16_t*>(v_out), stream));
+}
+
+size_t tgvkv_chunk_workspace_size(const tgvkv_problem* problem, const tgvkv_opts* opts, int32_t chunk) {
+    Shape s;
+    if (make_shape(problem, opts, &s) != TGVKV_OK || !chunk_fits(s, chunk)) return 0;
+    return align_up(tgvkv::chunk_workspace(s, chunk));
+}
+
+tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
+                                    const int32_t* block_table, int32_t max_pages, const int32_t* budgets,
+                                    int32_t decode_reserve, const int32_t* steps, const int32_t* n_new_or_null,
+                                    int32_t chunk, const void* q, const void* k_new, const void* v_new, void* out,
+                                    int32_t out_bf16, void* workspace, size_t workspace_bytes,
+                                    const int32_t* unit_order_or_null, hipStream_t stream) {
+    Shape s;
+    tgvkv_status st = make_shape(problem, opts, &s);
+    if (st != TGVKV_OK) return st;
+    tgvkv::Pages pg;
+    st = make_pages(pages, max_pages, block_table, &pg);
+    if (st != TGVKV_OK) return st;
+    if (decode_reserve < 0 || chunk < 1) return TGVKV_E_INVAL;
+    if (!chunk_fits(s, chunk)) return TGVKV_E_UNSUPPORTED;
+    if (s.B == 0) return TGVKV_OK;
+    if (!pages_present(pg) || budgets == nullptr || steps == nullptr || q == nullptr || k_new == nullptr ||
+        v_new == nullptr || out == nullptr)
+        return TGVKV_E_INVAL;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out)) return TGVKV_E_INVAL;
+    const size_t need = align_up(tgvkv::chunk_workspace(s, chunk));
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return TGVKV_E_WORKSPACE;
+    const tgvkv::Chunk ck{budgets, steps, n_new_or_null, decode_reserve, chunk, static_cast<const uint16_t*>(q),
+                          static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), out, out_bf16,
+                          unit_order_or_null, static_cast<float*>(workspace)};
+    return hip_status(tgvkv::launch_chunk(s, pg, ck, stream));
+}
+
+}  // extern "C"

@@ -97,4 +97,40 @@ hipError_t launch_decode_paged(const Shape& s, uint16_t* k_pool, uint16_t* v_poo
                                const uint16_t* k_new, const uint16_t* v_new, float* out, float* ws_part,
                                const int32_t* unit_order, hipStream_t st);
 
+// A pool of pages as the chunk and 8-bit calls see it: rows [n_pages][H_kv][2^shift][D] of `kind`
+// (TGVKV_CACHE_*), with 8-bit kinds also exponent bytes [n_pages][H_kv][2^shift]; and the segments' table.
+struct Pages {
+    uint8_t* k;
+    uint8_t* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+    int32_t n_pages, shift, kind;
+    const int32_t* table;  // [segments][max_pages]
+    int32_t max_pages;
+};
+
+hipError_t launch_compact_pages(const Shape& s, const Pages& pg, const uint16_t* k, const uint16_t* v,
+                                const int32_t* idx, const int32_t* budgets, const int64_t* idx_off, int64_t rows_total,
+                                const int32_t* unit_order, hipStream_t st);
+hipError_t launch_read_pages(const Shape& s, const Pages& pg, const int32_t* first, const int32_t* count,
+                             const int64_t* seg_off, uint16_t* kc, uint16_t* vc, hipStream_t st);
+
+// A call's new tokens: up to `chunk` per sequence, n_new[b] of them (null: all), from step steps[b] on.
+struct Chunk {
+    const int32_t* budgets;
+    const int32_t* steps;
+    const int32_t* n_new;
+    int32_t reserve, chunk;
+    const uint16_t* q;      // [B][L][chunk][H][D]
+    const uint16_t* k_new;  // [B][L][chunk][H_kv][D]
+    const uint16_t* v_new;
+    void* out;  // [B][L][chunk][H][D], f32 or bf16
+    int32_t out_bf16;
+    const int32_t* unit_order;
+    float* ws;
+};
+
+size_t chunk_workspace(const Shape& s, int32_t chunk);
+hipError_t launch_chunk(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st);
+
 }  // namespace tgvkv

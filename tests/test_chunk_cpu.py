@@ -1,0 +1,135 @@
+"""Refusals of the calls on pages of any kind, and the plain quantiser's own properties (no GPU)."""
+
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+from paper_2606_03075_amd import binding as bd
+from tests.pages_util import E4M3, bits, quantise, values
+from workloads import bf16_bits_to_f32
+
+
+def _gpu():
+    try:
+        import torch
+        return torch.cuda.is_available()
+    except Exception:
+        return False
+
+
+@pytest.fixture(scope="module")
+def so():
+    if not os.path.exists(bd.LIB_PATH):
+        from paper_2606_03075_amd import build
+        build.build()
+    return bd.load_library()
+
+
+def P(**kw):
+    base = dict(batch=1, layers=2, heads_q=4, heads_kv=2, head_dim=128, n_sys=3, n_vis=40, n_qst=5)
+    base.update(kw)
+    return bd.make_problem(**base)
+
+
+FAKE, ODD, BIG, S = 0x10000, 0x10008, 1 << 40, ctypes.c_void_p(0)
+
+
+def pages(k=FAKE, v=FAKE, ke=FAKE, ve=FAKE, n=64, size=8, kind=1):
+    return ctypes.byref(bd.TgvkvPages(k, v, ke, ve, n, size, kind))
+
+
+BAD_POOLS = [(dict(n=0), -1), (dict(n=1 << 31), -2), (dict(size=12), -1), (dict(size=0), -1), (dict(size=8192), -1),
+             (dict(kind=3), -1), (dict(kind=-1), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(k=ODD), -1),
+             (dict(ke=None), -1), (dict(ve=None, kind=2), -1), (dict(ve=ODD), -1)]
+
+
+@pytest.mark.skipif(_gpu(), reason="fake pointers are used only where no GPU exists")
+def test_chunk_refusals(so):
+    def go(problem=None, pool=pages(), table=FAKE, width=2, budgets=FAKE, reserve=4, steps=FAKE, chunk=3, q=FAKE, kn=FAKE,
+           vn=FAKE, out=FAKE, ws=FAKE, n=BIG, opts=None):
+        return so.tgvkv_chunk_attn_pages(ctypes.byref(problem or P()), opts, pool, table, width, budgets, reserve, steps,
+                                         None, chunk, q, kn, vn, out, 0, ws, n, None, S)
+    for bad, code in BAD_POOLS:
+        assert go(pool=pages(**bad)) == code, bad
+    assert go(pool=None) == -1
+    for bad, code in [(dict(table=None), -1), (dict(width=0), -1), (dict(width=5000), -2), (dict(budgets=None), -1),
+                      (dict(reserve=-1), -1), (dict(steps=None), -1), (dict(chunk=0), -1), (dict(chunk=-3), -1),
+                      (dict(chunk=1 << 30), -2), (dict(q=None), -1), (dict(kn=None), -1), (dict(vn=None), -1),
+                      (dict(out=None), -1), (dict(q=ODD), -1), (dict(kn=ODD), -1), (dict(vn=ODD), -1), (dict(out=ODD), -1),
+                      (dict(problem=P(head_dim=96)), -2), (dict(problem=P(heads_q=3)), -1),
+                      (dict(problem=P(heads_q=34)), -2), (dict(opts=ctypes.byref(bd.make_opts(head_mode=2))), -1)]:
+        assert go(**bad) == code, bad
+    need = bd.chunk_workspace_size(P(), None, 3)
+    if need:
+        assert go(ws=None) == -3 and go(n=need - 1) == -3 and go(ws=ODD) == -3
+    assert go(problem=P(batch=0), pool=pages(k=None), q=None, ws=None, n=0) == 0
+    assert so.tgvkv_chunk_attn_pages(None, None, pages(), FAKE, 2, FAKE, 4, FAKE, None, 3, FAKE, FAKE, FAKE, FAKE, 0, FAKE, BIG,
+                                     None, S) == -1
+
+
+@pytest.mark.skipif(_gpu(), reason="fake pointers are used only where no GPU exists")
+def test_store_and_read_refusals(so):
+    def store(problem=None, pool=pages(), k=FAKE, v=FAKE, idx=FAKE, budgets=FAKE, offs=FAKE, total=10, table=FAKE, width=2):
+        return so.tgvkv_compact_pages(ctypes.byref(problem or P()), None, k, v, idx, budgets, offs, total, pool, table, width,
+                                      None, S)
+
+    def read(problem=None, pool=pages(), table=FAKE, width=2, count=FAKE, seg=FAKE, k=FAKE, v=FAKE):
+        return so.tgvkv_read_pages(ctypes.byref(problem or P()), None, pool, table, width, None, count, seg, k, v, S)
+    for bad, code in BAD_POOLS:
+        assert store(pool=pages(**bad)) == code, bad
+        assert read(pool=pages(**bad)) == code, bad
+    assert store(pool=None) == read(pool=None) == -1
+    for bad, code in [(dict(k=None), -1), (dict(v=ODD), -1), (dict(idx=None), -1), (dict(budgets=None), -1),
+                      (dict(offs=None), -1), (dict(total=-1), -1), (dict(total=2 * 48 + 1), -4), (dict(width=1), -4),
+                      (dict(table=None), -1), (dict(problem=P(heads_q=3)), -1)]:
+        assert store(**bad) == code, bad
+        assert store(pool=pages(kind=0), **bad) == code, bad  # as tgvkv_compact_paged
+    for bad, code in [(dict(table=None), -1), (dict(width=0), -1), (dict(width=4097), -2), (dict(count=None), -1),
+                      (dict(seg=None), -1), (dict(k=None), -1), (dict(v=ODD), -1), (dict(problem=P(head_dim=32)), -2)]:
+        assert read(**bad) == code, bad
+    assert store(problem=P(batch=0), pool=pages(k=None)) == read(problem=P(batch=0), pool=pages(k=None)) == 0
+
+
+def test_chunk_workspace_size(so):
+    assert bd.chunk_workspace_size(P(head_dim=96), None, 1) == 0
+    assert bd.chunk_workspace_size(P(), None, 0) == 0
+    assert bd.chunk_workspace_size(P(), None, 1 << 30) == 0
+    for batch in (1, 7, 64):
+        for chunk in (1, 4, 64, 1000):
+            assert 0 <= bd.chunk_workspace_size(P(batch=batch, layers=32), None, chunk) <= 1 << 30
+
+
+def test_an_older_library_is_refused(tmp_path):
+    """A library without the calls on pages of any kind does not load."""
+    import subprocess
+    src = tmp_path / "old.c"
+    names = [n for n in bd.EXPORTS + bd.CEILING_EXPORTS if "pages" not in n]
+    src.write_text("".join(f"long {n}(void) {{ return {bd.ABI_VERSION if n == 'tgvkv_abi_version' else -1}; }}\n" for n in names))
+    lib = tmp_path / "libold.so"
+    r = subprocess.run(["gcc", "-shared", "-fPIC", "-o", str(lib), str(src)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    with pytest.raises(RuntimeError, match="rebuild"):
+        bd.load_library(str(lib))
+
+
+def test_plain_quantiser():
+    """The grid is e4m3's (torch's cast agrees on every code), the exponent is the least that fits, a row of its own
+    values is left as it is."""
+    import torch
+    assert np.array_equal(torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy(), E4M3, equal_nan=True)
+    rng = np.random.default_rng(0)
+    rows = bits(rng.standard_normal((50, 64)) * 2.0 ** rng.integers(-30, 30, (50, 1)))
+    x = bf16_bits_to_f32(rows).astype(np.float64)
+    for kind, most in ((bd.CACHE_FP8, 448.0), (bd.CACHE_INT8, 127.0)):
+        codes, exp = quantise(rows, kind)
+        unit = 2.0 ** (exp.astype(int) - 127)
+        amax = np.abs(x).max(-1)
+        assert np.all(amax <= most * unit) and np.all(amax > most * unit / 2)
+        v = values(codes, exp, kind)
+        again = quantise(bits(v), kind)
+        assert np.array_equal(values(*again, kind), v)
+        if kind == bd.CACHE_FP8:
+            y = torch.from_numpy((x / unit[:, None]).astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+            assert np.array_equal(y, codes)

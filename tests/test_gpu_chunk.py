@@ -1,0 +1,279 @@
+"""Chunk attention over pages of every kind on the GPU, against plain 64-bit forms.
+
+Head layouts, head dims, page sizes, kinds and result types; sequences that take no part, segments of no
+retained row, chunks of one token to many; padded tokens of NaN and unwritten rows of NaN (nothing of them may
+show); rows of out and pages that the call does not own, byte for byte.
+"""
+
+import numpy as np
+import pytest
+
+from paper_2606_03075_amd import binding as bd
+from tests.gpu_util import log
+from tests.pages_util import KINDS, call, case, check, parts, reference, tolerance
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(4, 4, 64), (2, 1, 128), (3, 1, 64), (7, 1, 128), (8, 1, 64), (16, 2, 64), (16, 1, 128), (10, 10, 128)]
+
+
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("chunk", [1, 2, 5, 33])
+def test_chunk_small(lib, hq, hkv, d, kind, chunk):
+    """Every head layout at ragged lengths around the tiles: no retained row, one, 15 to 17, 63 to 65, 200."""
+    log(f"chunk hq={hq} hkv={hkv} d={d} kind={kind} chunk={chunk}")
+    n_new = [chunk, 1, max(1, chunk - 1), 0, chunk]
+    c = case(hq * 100 + d + chunk, 5, 2, hq, hkv, d, chunk, kind, 16, [0, 1, 15, 17, 63, 65, 40, 40, 200, 129],
+             [0, 3, 0, 1, 2], n_new, chunk + 4)
+    check(c, out_bf16=bool(chunk & 1) and kind != bd.CACHE_BF16)
+
+
+@pytest.mark.parametrize("page", [1, 2, 8, 16, 64, 256, 4096])
+@pytest.mark.parametrize("kind", KINDS)
+def test_chunk_pages(lib, page, kind):
+    """Page sizes from one row to one page per segment; chunks that cross a page's end."""
+    log(f"chunk page={page} kind={kind}")
+    c = case(page, 2, 2, 6, 2, 128, 9, kind, page, [61, 120, 7, 255], [5, 0], [9, 8], 16)
+    check(c)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 4, 128), (7, 1, 64), (12, 4, 128)])
+@pytest.mark.parametrize("kind,out_bf16", [(bd.CACHE_BF16, False), (bd.CACHE_BF16, True), (bd.CACHE_FP8, True),
+                                           (bd.CACHE_INT8, False)])
+@pytest.mark.parametrize("chunk", [64, 150, 257])
+def test_chunk_long(lib, hq, hkv, d, kind, out_bf16, chunk):
+    """Chunks of several row tiles, their causal edge inside a key tile."""
+    log(f"chunk long hq={hq} hkv={hkv} d={d} kind={kind} bf16={out_bf16} chunk={chunk}")
+    c = case(chunk + d, 3, 1, hq, hkv, d, chunk, kind, 32, [70, 0, 333], [1, 0, 2], [chunk, chunk - 7, 1], chunk + 3)
+    check(c, out_bf16=out_bf16)
+
+
+@pytest.mark.parametrize("hq,hkv,d,chunk", [(1, 1, 128, 1), (7, 1, 128, 1), (4, 2, 64, 4), (7, 1, 128, 6)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_chunk_few_long_segments(lib, hq, hkv, d, chunk, kind):
+    """One or two long segments, where the work is split over the keys; lengths far apart."""
+    log(f"chunk few hq={hq} hkv={hkv} d={d} chunk={chunk} kind={kind}")
+    c = case(7 + chunk, 2, 1, hq, hkv, d, chunk, kind, 64, [6001, 37], [3, 2], None, chunk + 5)
+    check(c)
+    c = case(8 + chunk, 1, 1, hq, hkv, d, chunk, kind, 16, [2047], [0], None, chunk, order=False)
+    check(c, out_bf16=True)
+
+
+def test_chunk_many_layers_uneven(lib):
+    """Layers of very different budgets, some empty, in a given order."""
+    rng = np.random.default_rng(4)
+    b = np.minimum(rng.exponential(120, (3, 9)).astype(np.int32), 900)
+    b[:, 4] = 0
+    log("chunk uneven layers")
+    check(case(5, 3, 9, 8, 2, 128, 4, bd.CACHE_FP8, 16, b, [0, 9, 4], [4, 2, 3], 16))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_sequences_that_take_no_part(lib, kind):
+    """Idle, exhausted, empty and oversized counts; a table row too narrow for its segment's rows."""
+    log(f"chunk no part kind={kind}")
+    c = case(3, 7, 1, 4, 2, 64, 3, kind, 8, [20, 20, 20, 20, 20, 20, 0], [-1, 8, 6, 0, 0, 7, 0], [3, 1, 3, 0, 4, -2, 3], 8)
+    c["table"] = np.ascontiguousarray(c["table"][:, :3])  # 24 rows: 20 retained rows and 4 more
+    assert [n for _, n in parts(c)] == [0, 0, 0, 0, 0, 0, 3]
+    check(c)
+    c = case(4, 2, 2, 4, 2, 64, 3, kind, 8, [22, 10, 5, 21], [0, 0], None, 8)
+    c["table"] = np.ascontiguousarray(c["table"][:, :3])
+    assert [n for _, n in parts(c)] == [0, 3, 3, 3]
+    check(c)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("chunk", [6, 70])
+@pytest.mark.parametrize("where", ["k_new", "v_new", "q"])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_later_tokens_do_not_show(lib, kind, chunk, where, value):
+    """A non-finite value in a token's key, value or query leaves the tokens before it as they were."""
+    from tests.pages_util import bits
+    at = chunk - 3
+    log(f"chunk non-finite {where} {value} kind={kind} chunk={chunk}")
+    c = case(6, 2, 1, 6, 2, 128, chunk, kind, 16, [50, 3], [0, 1], None, chunk + 1)
+    c[where][:, :, at, :, 5] = bits(value)
+    before = case(6, 2, 1, 6, 2, 128, chunk, kind, 16, [50, 3], [0, 1], None, chunk + 1)
+    out, _ = call(c)
+    want, mag, qk = reference(before)
+    tol = tolerance(before, want, mag, qk, False)
+    assert np.all(np.abs(out - want)[:, :, :at] <= tol[:, :, :at])
+    if where == "q":  # nor the tokens after it
+        assert np.all(np.abs(out - want)[:, :, at + 1:] <= tol[:, :, at + 1:])
+        assert np.all(np.isnan(out[:, :, at]))
+    elif where == "v_new" and np.isnan(value):
+        g = c["hq"] // c["hkv"]
+        dims = [5] if kind == bd.CACHE_BF16 else list(range(c["d"]))
+        assert np.all(np.isnan(out[:, :, at:][..., dims])), g
+        if kind == bd.CACHE_BF16:  # the other dims keep their values
+            rest = [e for e in range(c["d"]) if e != 5]
+            assert np.all((np.abs(out - want) <= tol)[:, :, at:][..., rest])
+    elif where == "v_new" and kind == bd.CACHE_BF16:  # an infinity times its probability
+        got = out[:, :, at:, :, 5]
+        assert np.all(np.isnan(got) | (got == value)) and np.any(got == value)
+
+
+def test_extreme_logits(lib):
+    """Logits far apart (one key takes all), equal, and so low that a key of probability 0 has a value of 1e38."""
+    from tests.pages_util import bits
+    log("chunk extreme logits")
+    for spread in (8.0, 0.0):
+        check(case(9, 2, 2, 7, 1, 128, 5, bd.CACHE_BF16, 16, [100, 3, 64, 0], [0, 1], None, 8, spread=spread))
+    c = case(9, 1, 1, 4, 4, 64, 3, bd.CACHE_INT8, 16, [90], [0], None, 8)
+    c["k_new"][:, :, 0], c["q"][:] = bits(-30.0), bits(30.0)
+    c["v_new"][:, :, 0] = bits(1e38)
+    c["k_new"][:, :, 1:] = bits(30.0)
+    out, _ = call(c)
+    assert np.all(np.isfinite(out[:, :, 1:])) and np.abs(out[:, :, 1:]).max() < 10
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (7, 1)])
+def test_a_chunk_is_its_tokens_one_by_one(lib, kind, hq, hkv):
+    """The same tokens in one chunk, in two, and as decode steps: the same pages byte for byte, results within
+    the bound of two calls."""
+    import torch
+    log(f"chunk as steps kind={kind} hq={hq}")
+    c = case(11, 2, 3, hq, hkv, 128, 6, kind, 16, [33, 90, 5, 64, 200, 1], [0, 2], None, 9)
+    whole, pool = call(c)
+    got = np.full_like(whole, np.nan)
+    other = c["pool"].device()
+    for t in range(6):
+        s = dict(c, chunk=1, steps=c["steps"] + t, **{n: np.ascontiguousarray(c[n][:, :, t:t + 1]) for n in ("q", "k_new", "v_new")})
+        got[:, :, t:t + 1], _ = call(s, pool=other)
+    want, mag, qk = reference(c)
+    tol = tolerance(c, want, mag, qk, False)
+    assert np.all(np.abs(whole - want) <= tol) and np.all(np.abs(got - want) <= tol)
+    c["pool"].check(pool)
+    c["pool"].check(other)
+    if kind == bd.CACHE_BF16:  # and decode's own call on the same pool
+        fresh = case(11, 2, 3, hq, hkv, 128, 6, kind, 16, [33, 90, 5, 64, 200, 1], [0, 2], None, 9)
+        pool = fresh["pool"].device()
+        p = bd.make_problem(2, 3, hq, hkv, 128, 1, 0, 0)
+        ws = torch.zeros(max(1, bd.workspace_size(p, None, bd.CALL_DECODE)), dtype=torch.uint8, device="cuda")
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+        b16 = lambda a: up(a.view(np.int16)).view(torch.bfloat16)  # noqa: E731
+        out = torch.empty(2, 3, hq, 128, device="cuda")
+        for t in range(6):
+            pool.decode(p, None, up(c["table"]), up(c["budgets"]), 9, up(c["steps"] + t), b16(c["q"][:, :, t]),
+                        b16(c["k_new"][:, :, t]), b16(c["v_new"][:, :, t]), out, ws)
+            assert np.all(np.abs(out.double().cpu().numpy() - want[:, :, t]) <= tol[:, :, t])
+        c["pool"].check(pool)
+
+
+@pytest.mark.parametrize("kind", [bd.CACHE_BF16, bd.CACHE_INT8])
+def test_offsets_beyond_32_bits(lib, kind):
+    """Pages at the far end of a pool of more than 2^32 bytes."""
+    import torch
+    hkv, d, page = 8, 128, 128
+    n_pages = (1 << 32) // (hkv * d * page * (2 if kind == bd.CACHE_BF16 else 1)) + 64
+    log(f"chunk far pages kind={kind} n_pages={n_pages}")
+    c = case(12, 2, 1, 16, hkv, d, 5, kind, page, [200, 90], [0, 3], [5, 4], 16)
+    small = c["pool"].device()
+    big = bd.PagedPool(hkv, d, page, n_pages, kind=kind)
+    n = small.n_pages
+    for name in ("k_pool", "v_pool", "k_exp", "v_exp"):
+        t = getattr(small, name)
+        if t is not None:
+            as_bytes = lambda x: x.view(torch.int16) if kind == bd.CACHE_BF16 else x.view(torch.uint8)  # noqa: E731
+            as_bytes(getattr(big, name))[-n:] = as_bytes(t)
+    moved = dict(c, table=np.where(c["table"] >= 0, c["table"] + n_pages - n, -1).astype(np.int32))
+    out, _ = call(moved, pool=big)
+    want, mag, qk = reference(c)
+    there = ~np.isnan(want)
+    assert np.all(np.abs(out - want)[there] <= tolerance(c, want, mag, qk, False)[there])
+    for name in ("k_pool", "v_pool", "k_exp", "v_exp"):
+        if getattr(big, name) is not None:
+            setattr(big, name, getattr(big, name)[-n:])
+    c["pool"].check(big)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_without_a_page_are_not_written(lib, kind):
+    """Table entries outside the pool: nothing is written for their rows, and no page is disturbed."""
+    log(f"chunk rows without a page kind={kind}")
+    c = case(13, 1, 1, 4, 2, 64, 4, kind, 8, [7], [0], None, 16)
+    c["table"][0, 1] = -1  # rows 8 .. 15
+    out, pool = call(c)
+    for w, name in ((0, "k_new"), (1, "v_new")):
+        c["pool"].write(w, c["table"][0], 7, c[name][0, 0, 0])
+    c["pool"].check(pool)
+
+
+@pytest.mark.parametrize("hq,hkv,chunk,kind", [(4, 4, 3, bd.CACHE_FP8), (7, 1, 1, bd.CACHE_INT8), (7, 1, 4, bd.CACHE_BF16),
+                                               (4, 2, 80, bd.CACHE_BF16)])
+def test_graph_replays(lib, hq, hkv, chunk, kind):
+    """Two calls of different lengths on one workspace in one graph, replayed with eager calls of both between."""
+    import torch
+    log(f"chunk graph hq={hq} hkv={hkv} chunk={chunk} kind={kind}")
+    cases = [case(20, 1, 2, hq, hkv, 128, chunk, kind, 16, [3000, 411], [2], None, chunk + 2),
+             case(21, 2, 3, hq, hkv, 128, chunk, kind, 16, [40, 900, 0, 1500, 7, 77], [0, 1], None, chunk + 1)]
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    b16 = lambda a: up(a.view(np.int16)).view(torch.bfloat16)  # noqa: E731
+    probs = [bd.make_problem(c["B"], c["L"], hq, hkv, 128, 1, 0, 0) for c in cases]
+    ws = torch.full((max(1, *(bd.chunk_workspace_size(p, None, chunk) for p in probs)),), 255, dtype=torch.uint8, device="cuda")
+    calls = [(c["pool"].device(), p, (up(c["table"]), up(c["budgets"]), c["reserve"], up(c["steps"]), None, b16(c["q"]),
+                                      b16(c["k_new"]), b16(c["v_new"]), torch.empty(c["q"].shape, device="cuda"), ws))
+             for c, p in zip(cases, probs)]
+
+    def step(x):
+        x[0].extend(x[1], None, *x[2])
+    want = []
+    for x in calls:
+        ws.fill_(255)
+        step(x)
+        want.append(x[2][8].clone())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x in calls + calls[:1]:
+            step(x)
+    for rep in range(4):
+        for x in calls:
+            x[2][8].fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x[2][8], w) for x, w in zip(calls, want)), rep
+        x = calls[rep % 2]
+        x[2][8].fill_(float("nan"))
+        step(x)
+        torch.cuda.synchronize()
+        assert torch.equal(x[2][8], want[rep % 2]), rep
+
+
+def test_other_streams(lib):
+    """Two calls at once, each on a stream of its own with a workspace of its own, and the stream argument."""
+    import torch
+    log("chunk on two streams")
+    cs = [case(30 + i, 2, 2, 7, 1, 128, 3, bd.CACHE_FP8, 16, [1500, 20, 300, 900], [0, 1], None, 8) for i in range(2)]
+    refs = []
+    for c in cs:
+        pool = c["pool"].device()
+        refs.append((pool, *reference(c)))
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    b16 = lambda a: up(a.view(np.int16)).view(torch.bfloat16)  # noqa: E731
+    p = bd.make_problem(2, 2, 7, 1, 128, 1, 0, 0)
+    args = [(up(c["table"]), up(c["budgets"]), 8, up(c["steps"]), None, b16(c["q"]), b16(c["k_new"]), b16(c["v_new"]),
+             torch.empty(c["q"].shape, device="cuda"),
+             torch.empty(max(1, bd.chunk_workspace_size(p, None, 3)), dtype=torch.uint8, device="cuda")) for c in cs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        with torch.cuda.stream(streams[0]):
+            refs[0][0].extend(p, None, *args[0])
+        refs[1][0].extend(p, None, *args[1], stream=streams[1])
+    torch.cuda.synchronize()
+    for c, a, (pool, want, mag, qk) in zip(cs, args, refs):
+        assert np.all(np.abs(a[8].double().cpu().numpy() - want) <= tolerance(c, want, mag, qk, False))
+        c["pool"].check(pool)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_repeated_calls_give_the_same_bits(lib, kind):
+    import torch
+    log(f"chunk repeat kind={kind}")
+    c = case(40, 2, 2, 7, 1, 128, 5, kind, 16, [2500, 90, 700, 3], [0, 1], None, 8)
+    first, _ = call(c)
+    for _ in range(3):
+        assert np.array_equal(call(c)[0], first)
+    torch.cuda.synchronize()
