@@ -81,6 +81,12 @@ __device__ __forceinline__ f32x4 mfma16x16x16(bf16x4 a, bf16x4 b, f32x4 c) {
                                                      0, 0, 0);
 }
 
+// LDS read that transposes 16-bit elements: in each group of 16 lanes, lane i gives the address of 4 elements of
+// row i / 4 (columns 4 (i % 4) ..), and gets column i of the group's 4 rows.
+__device__ __forceinline__ s16x4 lds_read_tr16(const void* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
+}
+
 template <typename T>
 __device__ __forceinline__ T shfl_xor(T v, int mask) {
     return __shfl_xor(v, mask, 64);

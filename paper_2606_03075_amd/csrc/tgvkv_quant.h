@@ -117,6 +117,25 @@ __device__ __forceinline__ u32x4 decode8(u32x2 c) {
     return u32x4{a[0], a[1], b[0], b[1]};
 }
 
+// 4 codes as the 4 bf16 that they stand for, s = 2^e of their row (byte 255: s is inf, 0 * inf = NaN).
+template <int KIND>
+__device__ __forceinline__ u32x2 values4(uint32_t w, float s) {
+    float f[4];
+    if (KIND == kCacheFp8) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        f[0] = lo[0] * s;
+        f[1] = lo[1] * s;
+        f[2] = hi[0] * s;
+        f[3] = hi[1] * s;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = (float)(int8_t)(w >> (8 * j)) * s;
+    }
+    return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+                 __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
+}
+
 // 2 bf16 times a power of two, as bf16 (exact in the normal range; inf * 0 = NaN for the byte 255).
 __device__ __forceinline__ uint32_t scale2bf16(uint32_t w, float s) {
     return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(w & 0xFFFF0000u) * s),
