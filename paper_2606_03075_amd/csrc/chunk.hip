@@ -38,7 +38,6 @@ namespace tgvkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCUs = 256;
 
 // One segment's part in the call: its first new row and its new tokens, 0 where it takes no part (an idle
 // or exhausted sequence, or a table row too narrow for the rows).
@@ -82,10 +81,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Shape s, Pages pg, Chu
     }
 }
 
-template <int D>
-constexpr int kKRow = D * 2 + 16;  // LDS bytes of a staged K row
-template <int D>
-constexpr int kVRow = D * 2 + 32;  // and of a V row
+// LDS rows of a block of keys.  bf16: K rows padded by 16 bytes (a read takes one column of 16 rows), V rows by 32
+// (a transposing read takes 32 bytes of 8 rows).  Codes: both by 16, and the upper 16 V rows 16 further.
+template <int D, bool CODES>
+struct Block {
+    static constexpr int K = CODES ? D + 16 : D * 2 + 16;
+    static constexpr int V = CODES ? D + 16 : D * 2 + 32;
+    __device__ static int k_at(int row) { return row * K; }
+    __device__ static int v_at(int row) { return row * V + (CODES && row >= 16 ? 16 : 0); }
+    static constexpr int kBytes = 32 * K, vBytes = 32 * V + (CODES ? 16 : 0);  // of 32 rows
+};
 
 // A lane's 16 bytes of bf16 with what is not finite set to 0; true if there was any.
 __device__ __forceinline__ bool drop_non_finite(u32x4& r) {
@@ -99,13 +104,20 @@ __device__ __forceinline__ bool drop_non_finite(u32x4& r) {
     return any;
 }
 
-// 16 NT query rows of one (segment, KV head) in a wave, row 16 nt + l % 16 in lane l.
-template <int D, int NT, bool FINE>
+// 16 NT query rows of one (segment, KV head) in a wave, row 16 nt + l % 16 in lane l.  Keys come as bf16 rows in LDS
+// (CODED = kCacheBf16) or as codes of that kind with their rows' powers of two beside them.  PARTS: bf16 parts of
+// a probability in the product with V.
+template <int D, int NT, int PARTS, int CODED>
 struct QueryRows {
+    static constexpr bool CODES = CODED != kCacheBf16;
+    using B = Block<D, CODES>;
     bf16x8 qf[NT][D / 32];  // B operand of S^T: 8 dims of the lane's quarter per step
     f32x4 o[NT][D / 16];    // O^T: dims 16 db + 4 (l / 16) + {0..3}
     float m[NT], l[NT];     // running maximum (base-2 logits) and the lane quarter's share of the sum
     int lim[NT];            // last visible row
+
+    // First of the 8 dims of step ks in lane quarter qq.  A read of 16 codes feeds two steps.
+    __device__ static int dim_of(int ks, int qq) { return CODES ? 64 * (ks / 2) + 16 * qq + 8 * (ks % 2) : 32 * ks + 8 * qq; }
 
     // Rows r0 .. of the c G rows; rows behind the last are zeros and see what the last one sees.
     __device__ __forceinline__ void load(const Shape& s, const Chunk& ck, const Part& part, int bl, int kvh, int r0) {
@@ -115,10 +127,10 @@ struct QueryRows {
             const int r = r0 + nt * 16 + c, rows = part.count * s.G;
             const bool in = r < rows;
             const int i = min(r, rows - 1) / s.G, g = min(r, rows - 1) % s.G;
-            const uint16_t* qp = ck.q + (((size_t)bl * ck.chunk + i) * s.H + kvh * s.G + g) * D + qq * 8;
+            const uint16_t* qp = ck.q + (((size_t)bl * ck.chunk + i) * s.H + kvh * s.G + g) * D;
             const u32x4 z = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) qf[nt][ks] = as_bf16x8(in ? load16(qp + ks * 32) : z);
+            for (int ks = 0; ks < D / 32; ++ks) qf[nt][ks] = as_bf16x8(in ? load16(qp + dim_of(ks, qq)) : z);
             lim[nt] = part.first + i;
             m[nt] = kNegInf;
             l[nt] = 0.f;
@@ -133,32 +145,59 @@ struct QueryRows {
             for (int ks = 0; ks < D / 32; ++ks) settle(qf[nt][ks]);
     }
 
-    // One step over the 32 staged rows n0 ..; MASK: only those up to lim count, and below `end`.
+    // One step over the 32 staged rows n0 ..; MASK: only those up to lim count, and below `end`.  scales: with codes,
+    // the rows' powers of two, 32 of K and 32 of V.
     template <bool MASK>
-    __device__ __forceinline__ void step(const char* kst, const char* vst, int n0, int end, float scale2) {
+    __device__ __forceinline__ void step(const char* kst, const char* vst, const float* scales, int n0, int end, float scale2) {
         const int c = threadIdx.x & 15, qq = (threadIdx.x & 63) >> 4;
         f32x4 a[2][NT];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) a[b][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const char *kp0 = kst + B::k_at(c) + qq * 16, *kp1 = kst + B::k_at(16 + c) + qq * 16;
+        if constexpr (CODES) {
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) {
-            const bf16x8 k0 = as_bf16x8(load16(kst + c * kKRow<D> + ks * 64 + qq * 16));
-            const bf16x8 k1 = as_bf16x8(load16(kst + (16 + c) * kKRow<D> + ks * 64 + qq * 16));
+            for (int kp = 0; kp < D / 64; ++kp) {
+                const u32x4 w0 = load16(kp0 + kp * 64), w1 = load16(kp1 + kp * 64);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                a[0][nt] = mfma16x16x32(k0, qf[nt][ks], a[0][nt]);
-                a[1][nt] = mfma16x16x32(k1, qf[nt][ks], a[1][nt]);
+                for (int h = 0; h < 2; ++h) {
+                    const bf16x8 k0 = as_bf16x8(decode8<CODED>(u32x2{w0[2 * h], w0[2 * h + 1]}));
+                    const bf16x8 k1 = as_bf16x8(decode8<CODED>(u32x2{w1[2 * h], w1[2 * h + 1]}));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        a[0][nt] = mfma16x16x32(k0, qf[nt][2 * kp + h], a[0][nt]);
+                        a[1][nt] = mfma16x16x32(k1, qf[nt][2 * kp + h], a[1][nt]);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                const bf16x8 k0 = as_bf16x8(load16(kp0 + ks * 64)), k1 = as_bf16x8(load16(kp1 + ks * 64));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    a[0][nt] = mfma16x16x32(k0, qf[nt][ks], a[0][nt]);
+                    a[1][nt] = mfma16x16x32(k1, qf[nt][ks], a[1][nt]);
+                }
             }
         }
-        bf16x8 ph[NT], pl[FINE ? NT : 1];
+        f32x4 ksc[2], vsc[2];
+        if constexpr (CODES) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                ksc[b] = *reinterpret_cast<const f32x4*>(scales + 16 * b + 4 * qq);
+                vsc[b] = *reinterpret_cast<const f32x4*>(scales + 32 + 16 * b + 4 * qq);
+            }
+        }
+        bf16x8 pp[PARTS][NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float z[8], mb = kNegInf;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 z[j] = a[j / 4][nt][j % 4];
+                if constexpr (CODES) z[j] *= ksc[j / 4][j % 4];
                 if (MASK) {
                     const int n = n0 + 16 * (j / 4) + 4 * qq + j % 4;
                     z[j] = n <= lim[nt] && n < end ? z[j] : kNegInf;
@@ -176,23 +215,34 @@ struct QueryRows {
             const float mu = m[nt] == kNegInf ? 0.f : m[nt];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p = fast_exp2(__builtin_fmaf(z[j], scale2, -mu));
+                float p = fast_exp2(__builtin_fmaf(z[j], scale2, -mu));
                 l[nt] += p;
-                ph[nt][j] = (__bf16)p;
-                if (FINE) pl[nt][j] = (__bf16)(p - (float)ph[nt][j]);
+                if constexpr (CODES) p *= vsc[j / 4][j % 4];
+                pp[0][nt][j] = (__bf16)p;
+#pragma unroll
+                for (int x = 1; x < PARTS; ++x) {
+                    p -= (float)pp[x - 1][nt][j];
+                    pp[x][nt][j] = (__bf16)p;
+                }
             }
         }
-        const char* vp = vst + (4 * qq + (c >> 2)) * kVRow<D> + (c & 3) * 8;
+        // keys of a lane's slots: 4 qq + {0..3}, 16 + 4 qq + {0..3}
+        const char* vp = CODES ? vst + B::v_at((c >> 1) < 4 ? 4 * qq + (c >> 1) : 12 + 4 * qq + (c >> 1)) + (c & 1) * 8
+                               : vst + B::v_at(4 * qq + (c >> 2)) + (c & 3) * 8;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
-            const s16x4 v0 = lds_read_tr16(vp + db * 32), v1 = lds_read_tr16(vp + 16 * kVRow<D> + db * 32);
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const bf16x8 vv = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                o[nt][db] = mfma16x16x32(vv, ph[nt], o[nt][db]);
-                if (FINE) o[nt][db] = mfma16x16x32(vv, pl[nt], o[nt][db]);
+            bf16x8 vv;
+            if constexpr (CODES) {
+                vv = as_bf16x8(decode8<CODED>(__builtin_bit_cast(u32x2, lds_read_tr8(vp + db * 16))));
+            } else {
+                typedef short s16x8 __attribute__((ext_vector_type(8)));
+                const s16x4 v0 = lds_read_tr16(vp + db * 32), v1 = lds_read_tr16(vp + 16 * B::V + db * 32);
+                vv = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x) o[nt][db] = mfma16x16x32(vv, pp[x][nt], o[nt][db]);
         }
     }
 
@@ -205,7 +255,7 @@ struct QueryRows {
     // Adds the non-finite values of V rows n0 .. n1 - 1 that a row sees: those of the new tokens in bf16, or, with
     // 8-bit pages, rows of the exponent byte 255.
     template <int KIND>
-    __device__ __forceinline__ void add_non_finite(const Shape& s, const Pages& pg, const Chunk& ck, const Part& part, int bl,
+    __device__ __forceinline__ void add_non_finite(const Shape& s, const Chunk& ck, const Part& part, int bl,
                                                    int kvh, int n0, int n1) {
         const int qq = (threadIdx.x & 63) >> 4;
         for (int n = n0; n < n1; ++n) {
@@ -231,25 +281,6 @@ struct QueryRows {
     }
 };
 
-// 8 values of a new row as later steps will read them, and the row into its page.
-template <int D, int KIND>
-__device__ __forceinline__ u32x4 append8(const Pages& pg, uint8_t* pool, uint8_t* exps, size_t row, int cc, bool in, u32x4 r) {
-    if constexpr (KIND == kCacheBf16) {
-        if (in) store16(pool + (row * D + cc * 8) * 2, r);
-        return r;
-    } else {
-        const uint32_t e = exp_byte<KIND>(group_max<D / 8>(amax8(r)));
-        const u32x2 codes = encode8<KIND>(r, e);
-        if (in) {
-            *reinterpret_cast<u32x2*>(pool + row * D + cc * 8) = codes;
-            if (cc == 0) exps[row] = (uint8_t)e;
-        }
-        const float sc = exp_scale(e);
-        const u32x2 a = values4<KIND>(codes[0], sc), b = values4<KIND>(codes[1], sc);
-        return u32x4{a[0], a[1], b[0], b[1]};
-    }
-}
-
 // Rows of a segment's pages: the first pool row of every page of rows [n0, n1), in LDS.  A pool's rows are
 // numbered in 32 bits (2^32 of the smallest rows, in two pools, are more memory than the GPU has).
 struct PageRows {
@@ -266,58 +297,141 @@ struct PageRows {
     __device__ __forceinline__ size_t row(int n) const { return base[(n >> shift) - p0] + (uint32_t)(n & ((1 << shift) - 1)); }
 };
 
-// One lane's share of `ROWS` rows' K or V on its way from the pages to LDS.  LANES lanes work together, each on 16
+// One lane's share of `ROWS` rows' K or V on its way from the pages.  LANES lanes work together, each on 16
 // bytes of a row at a time: 8 bf16, or 16 codes.
 template <int D, int KIND, int ROWS, int LANES>
 struct Staged {
     static constexpr int CH = D * code_bytes(KIND) / 16;  // 16-byte pieces per row
     static constexpr int N = ROWS * CH / LANES;
     u32x4 x[N];
-    uint32_t e[KIND == kCacheBf16 ? 1 : N];
-
     __device__ __forceinline__ static int row_of(int it, int lane) { return (it * LANES + lane) / CH; }
-
-    __device__ __forceinline__ void from_page(int it, int lane, const uint8_t* pool, const uint8_t* exps, size_t row) {
-        x[it] = load16_stream(pool + (row * CH + (it * LANES + lane) % CH) * 16);
-        if constexpr (KIND != kCacheBf16) e[it] = exps[row];
-    }
-    // To LDS rows of `stride` bytes, as bf16.
-    __device__ __forceinline__ void store(int it, int lane, char* lds, int stride) {
-        char* p = lds + row_of(it, lane) * stride + (it * LANES + lane) % CH * (KIND == kCacheBf16 ? 16 : 32);
-        if constexpr (KIND == kCacheBf16) {
-            store16(p, x[it]);
-        } else {
-            const float sc = exp_scale(e[it]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x2 a = values4<KIND>(x[it][2 * h], sc), b = values4<KIND>(x[it][2 * h + 1], sc);
-                store16(p + 16 * h, u32x4{a[0], a[1], b[0], b[1]});
-            }
-        }
+    __device__ __forceinline__ static int piece_of(int it, int lane) { return (it * LANES + lane) % CH; }
+    __device__ __forceinline__ void load(int it, int lane, const uint8_t* pool, size_t row) {
+        x[it] = load16_stream(pool + (row * CH + piece_of(it, lane)) * 16);
     }
 };
 
 // Results of a row: f32 or bf16.
-template <bool FINE>
+template <int PARTS>
 __device__ __forceinline__ void store_out(const Chunk& ck, size_t at, float v) {
-    if constexpr (FINE) reinterpret_cast<float*>(ck.out)[at] = v;
+    if constexpr (PARTS > 1) reinterpret_cast<float*>(ck.out)[at] = v;
     else reinterpret_cast<__bf16*>(ck.out)[at] = (__bf16)v;
 }
 
-// Splits of a unit's keys over workgroups, joined in the same launch: each workgroup of a unit leaves its
-// partial and then a mark, the call's number, and the one that finds every mark joins the partials in split order and
-// clears the marks.  No workgroup waits.  Partials and marks are GPU-scope atomic accesses, which
-// go through to memory, so that a finished store is visible on every XCD.  The workspace's first contents
-// do not matter: a mark counts only if it is this call's number, 64 bits that differ between calls; a
-// replayed graph brings its number again, but every call leaves its marks cleared.
-struct KeySplits {
-    unsigned long long* marks;  // [units][most]
-    float* part;                // [units][most][rows][D + 2]
+// Shares of the keys.  An item is the work of one (segment, KV head, row tile).  Segments differ in length
+// by an order of magnitude, and a call may have few of them, so a long item is cut into shares of S rows: its first share
+// has the item's own workgroup, the others take the call's `extras` workgroups, which come first in
+// the grid.  S = the call's rows over its extras, so that these suffice whatever the lengths are, and at least
+// kShareRows.  A workgroup finds its share from the segments' lengths (a scan of at most kScanSegments; an item of
+// up to kShareRows needs none).  Calls of more items have no extras and every item is whole.
+//
+// The shares of an item are joined in the same launch: each leaves its partial (maximum, sum, weighted sum per
+// row) and then a mark, the call's number; the one that finds every mark joins the partials in order and clears
+// the marks.  No workgroup waits.  Partials and marks are GPU-scope atomic accesses, which go through to memory, so
+// that a finished store is visible on every XCD.  The workspace's first contents do not matter: a mark counts
+// only if it is this call's number, 64 bits that differ between calls; a replayed graph brings its number again,
+// but every call leaves its marks cleared.
+struct Shares {
+    unsigned long long* marks;  // [2 extras]
+    float* part;                // [2 extras][rows][D + 2]
     unsigned long long call;
-    int most;
+    int extras;
 };
-constexpr int kMaxKeySplits = 32;
-constexpr int kSplitRows = 256;  // a split has at least so many rows
+constexpr int kShareRows = 256;
+constexpr int kMaxShares = 16;  // of an item
+constexpr int kScanSegments = 2048;
+
+struct Item {
+    int bl, kvh, tile;
+    int share, shares, rows;  // its share, shares of the item, rows per share
+    int slot0;                // slots of the item: slot0 + {0 .. shares - 2} its extras, extras + slot0 its first share
+    __device__ int slot(int i, int extras) const { return i == 0 ? extras + slot0 : slot0 + i - 1; }
+};
+
+__device__ __forceinline__ int rows_per_share(int len, int least) {
+    return max(least, ((len + kMaxShares - 1) / kMaxShares + 63) / 64 * 64);
+}
+
+// The item and share of a workgroup; false: none.  `item` is the workgroup's own item where it is not an extra.  Called by
+// all threads, with the same arguments.
+__device__ __forceinline__ bool take_share(const Shape& s, const Pages& pg, const Chunk& ck, const Shares& sh, int tiles,
+                                           int units, int unit, int tile, Item& it) {
+    __shared__ unsigned long long total_w[4];
+    __shared__ int extra_w[4], found[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool extra = (int)blockIdx.x < sh.extras;
+    if (!extra) {
+        if (unit >= units) return false;
+        it.kvh = unit % s.Hkv;
+        it.bl = ck.unit_order != nullptr ? min(max(ck.unit_order[unit / s.Hkv], 0), s.B * s.L - 1) : unit / s.Hkv;
+        it.tile = tile;
+        it.share = 0;
+        it.shares = 1;
+        it.slot0 = 0;
+        const Part part = part_of(s, pg, ck, it.bl);
+        it.rows = part.first + part.count;
+        if (part.count == 0) return false;
+        if (sh.extras == 0 || it.rows <= kShareRows) return true;
+    }
+    // every thread has the segments of its own run
+    const int n = s.B * s.L, per = (n + kThreads - 1) / kThreads, heads = s.Hkv * tiles;
+    const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
+    unsigned long long total = 0;
+    for (int i = i0; i < i1; ++i) {
+        const Part p = part_of(s, pg, ck, i);
+        total += (unsigned)(p.first + p.count);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+    if (lane == 0) total_w[wave] = total;
+    if (tid == 0) found[0] = -1;
+    __syncthreads();
+    total = (total_w[0] + total_w[1] + total_w[2] + total_w[3]) * (unsigned)heads;
+    const int least = (int)min((total / (unsigned)sh.extras + 64) / 64 * 64, 1ull << 30);
+    const int rows0 = max(kShareRows, least);
+    int mine = 0;  // extras of the thread's run
+    for (int i = i0; i < i1; ++i) {
+        const Part p = part_of(s, pg, ck, i);
+        const int len = p.first + p.count;
+        if (len > rows0) mine += ((len - 1) / rows_per_share(len, rows0)) * heads;
+    }
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(before, o);
+        if (lane >= o) before += y;
+    }
+    if (lane == 63) extra_w[wave] = before;
+    __syncthreads();
+    before -= mine;
+    for (int w = 0; w < wave; ++w) before += extra_w[w];
+    for (int i = i0; i < i1; ++i) {
+        const Part p = part_of(s, pg, ck, i);
+        const int len = p.first + p.count;
+        const int k = len > rows0 ? (len - 1) / rows_per_share(len, rows0) : 0;
+        const int x = (int)blockIdx.x - before;
+        if (extra ? x >= 0 && x < k * heads : i == it.bl) {
+            found[0] = i;
+            found[1] = k + 1;
+            found[2] = before;
+            found[3] = rows_per_share(len, rows0);
+        }
+        before += k * heads;
+    }
+    __syncthreads();
+    if (found[0] < 0) return false;
+    it.shares = found[1];
+    it.rows = found[3];
+    if (extra) {
+        const int x = (int)blockIdx.x - found[2], k = it.shares - 1;
+        it.bl = found[0];
+        it.kvh = x / k / tiles;
+        it.tile = x / k % tiles;
+        it.share = 1 + x % k;
+    }
+    it.slot0 = found[2] + (it.kvh * tiles + it.tile) * (it.shares - 1);
+    return true;
+}
 
 __device__ __forceinline__ void store_shared(float* p, float v) {
     __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -326,84 +440,175 @@ __device__ __forceinline__ float load_shared(const float* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int D, int KIND, int NT, bool FINE>
-__global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk ck, KeySplits sp) {
-    constexpr int KB = 32;               // keys per block
+// Called by all threads of a workgroup after they wrote its share's partial of `rows` rows (of at most ROWS); the last
+// to come joins them.  ml: LDS of 2 ROWS kMaxShares floats.  r0: the tile's first query row.
+template <int D, int ROWS, int PARTS>
+__device__ __forceinline__ void join_shares(const Shape& s, const Chunk& ck, const Shares& sh, const Item& it, int rows, int r0,
+                                            float* ml) {
+    __shared__ int all_here;
+    const int tid = threadIdx.x, n = it.shares;
+    wait_vmem_ordered();  // this thread's part of the partial has reached memory ...
+    __syncthreads();      // ... and every thread's has, before the mark
+    if (tid < 64) {
+        if (tid == 0)
+            __hip_atomic_store(sh.marks + it.slot(it.share, sh.extras), sh.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        wait_vmem_ordered();  // the mark has reached memory before the others' are read
+        const bool here = tid >= n || __hip_atomic_load(sh.marks + it.slot(min(tid, n - 1), sh.extras), __ATOMIC_RELAXED,
+                                                        __HIP_MEMORY_SCOPE_AGENT) == sh.call;
+        const bool all = __ballot(!here) == 0;
+        if (tid == 0) all_here = all;
+    }
+    __syncthreads();
+    if (!all_here) return;
+    for (int x = tid; x < rows * n; x += kThreads) {  // maxima and sums to LDS
+        const int r = x / n, i = x % n;
+        const float* p = sh.part + ((size_t)it.slot(i, sh.extras) * ROWS + r) * (D + 2);
+        ml[r * kMaxShares + i] = load_shared(p);
+        ml[(ROWS + r) * kMaxShares + i] = load_shared(p + 1);
+    }
+    __syncthreads();
+    for (int x = tid; x < rows * D; x += kThreads) {
+        const int r = x / D, e = x % D;
+        float a[kMaxShares], M = kNegInf;
+#pragma unroll
+        for (int i = 0; i < kMaxShares; ++i)
+            a[i] = load_shared(sh.part + ((size_t)it.slot(min(i, n - 1), sh.extras) * ROWS + r) * (D + 2) + 2 + e);
+        for (int i = 0; i < n; ++i) M = fmaxf(M, ml[r * kMaxShares + i]);
+        const float mu = M == kNegInf ? 0.f : M;
+        float num = 0.f, den = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMaxShares; ++i) {
+            if (i < n) {
+                const float sc = fast_exp2(ml[r * kMaxShares + i] - mu);
+                num += sc * a[i];
+                den += sc * ml[(ROWS + r) * kMaxShares + i];
+            }
+        }
+        const int q = r0 + r;
+        store_out<PARTS>(ck, (((size_t)it.bl * ck.chunk + q / s.G) * s.H + it.kvh * s.G + q % s.G) * D + e, num / den);
+    }
+    if (tid < n)
+        __hip_atomic_store(sh.marks + it.slot(tid, sh.extras), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int D, int KIND, int NT, int PARTS>
+__global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk ck, Shares sh) {
+    constexpr bool CODES = KIND != kCacheBf16;
+    using B = Block<D, CODES>;
+    constexpr int KB = 32;  // keys per block
     constexpr int ROWS = 16 * NT;
-    constexpr int CPR = D / 8;           // 16-byte pieces of a bf16 row
-    constexpr int STAGE = KB * (kKRow<D> + kVRow<D>);
+    constexpr int CPR = D / 8;  // 16-byte pieces of a bf16 row
+    constexpr int STAGE = (B::kBytes + B::vBytes + (CODES ? 64 * (int)sizeof(float) : 0) + 15) / 16 * 16;
     constexpr int MERGE = 4 * ROWS * (D + 2) * (int)sizeof(float);
+    static_assert(MERGE >= 2 * ROWS * kMaxShares * (int)sizeof(float), "room to join the shares");
     __shared__ __align__(16) char smem[4 * STAGE > MERGE ? 4 * STAGE : MERGE];
     extern __shared__ uint32_t lds_pages[];
-    __shared__ int found;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int split = blockIdx.x % sp.most, slot = blockIdx.x / sp.most;
-    const int kvh = slot % s.Hkv;
-    const int bl = ck.unit_order != nullptr ? min(max(ck.unit_order[slot / s.Hkv], 0), s.B * s.L - 1) : slot / s.Hkv;
+    Item it;
+    const int units = s.B * s.L * s.Hkv;
+    if (!take_share(s, pg, ck, sh, 1, units, (int)blockIdx.x - sh.extras, 0, it)) return;
+    const int bl = it.bl, kvh = it.kvh;
     const Part part = part_of(s, pg, ck, bl);
-    if (part.count == 0) return;
     const int f = part.first, c = part.count, rows = c * s.G;
-    const int nsplit = min(max((f + kSplitRows - 1) / kSplitRows, 1), sp.most);
-    if (split >= nsplit) return;
-    const int per = ((f + KB - 1) / KB + nsplit - 1) / nsplit * KB;
-    const int t0 = min(split * per, f), t1 = min(t0 + per, f);
+    const bool last_share = it.share == it.shares - 1;  // takes the new rows
+    const int t0 = min(it.share * it.rows, f), t1 = it.shares == 1 ? f : min(t0 + it.rows, f);
     PageRows pages;
     pages.init(s, pg, bl, kvh, t0, t1, lds_pages);
     __syncthreads();
 
     char* kst = smem + wave * STAGE;
-    char* vst = kst + KB * kKRow<D>;
+    char* vst = kst + B::kBytes;
+    float* scales = reinterpret_cast<float*>(kst + (B::kBytes + B::vBytes + 15) / 16 * 16);
     Staged<D, KIND, KB, 64> ka, va;
+    uint32_t ex = 0;  // codes: exponent byte of K row `lane`, or of V row `lane` - 32
     // rows behind the last repeat it (they count nothing), so every load is issued
     auto issue = [&](int n0) {
 #pragma unroll
-        for (int it = 0; it < ka.N; ++it) {
-            const size_t row = pages.row(min(n0 + ka.row_of(it, lane), t1 - 1));
-            ka.from_page(it, lane, pg.k, pg.k_exp, row);
-            va.from_page(it, lane, pg.v, pg.v_exp, row);
+        for (int i = 0; i < ka.N; ++i) {
+            const size_t row = pages.row(min(n0 + ka.row_of(i, lane), t1 - 1));
+            ka.load(i, lane, pg.k, row);
+            va.load(i, lane, pg.v, row);
         }
+        if constexpr (CODES) ex = (lane < 32 ? pg.k_exp : pg.v_exp)[pages.row(min(n0 + (lane & 31), t1 - 1))];
     };
+    const int blocks = (t1 - t0 + KB - 1) / KB;
     int n0 = t0 + KB * wave;
     if (n0 < t1) issue(n0);
-    QueryRows<D, NT, FINE> qr;
+    QueryRows<D, NT, PARTS, KIND> qr;
     qr.load(s, ck, part, bl, kvh, 0);
     qr.settle_rows();
 
-    // the new rows, a block of their own: to the pages, and attended as the pages hold them
-    if (split == nsplit - 1 && wave == 3) {
+    // the new rows, a block of their own for the wave that would take the next one: to the pages, and attended as
+    // the pages hold them
+    if (last_share && wave == (blocks & 3)) {
         const int cc = lane % CPR;
         bool odd = false;
-#pragma unroll 4
-        for (int it = 0; it < KB * CPR / 64; ++it) {
-            const int i = it * (64 / CPR) + lane / CPR, n = f + min(i, c - 1);
-            const size_t src = (((size_t)bl * ck.chunk + min(i, c - 1)) * s.Hkv + kvh) * D + cc * 8;
-            u32x4 kr = load16(ck.k_new + src), vr = load16(ck.v_new + src);
-            const int page = table_page(pg, bl, n);
-            const bool in = i < c && page >= 0 && page < pg.n_pages;  // a row without a page is not written
-            const size_t row = pool_row(pg, s.Hkv, kvh, page, n);
-            kr = append8<D, KIND>(pg, pg.k, pg.k_exp, row, cc, in, kr);
-            vr = append8<D, KIND>(pg, pg.v, pg.v_exp, row, cc, in, vr);
-            odd |= drop_non_finite(vr);
-            store16(kst + i * kKRow<D> + cc * 16, kr);
-            store16(vst + i * kVRow<D> + cc * 16, vr);
+        for (int i0 = 0; i0 < KB; i0 += 64 / CPR) {
+            const int i = i0 + lane / CPR;
+            u32x4 kr = {0u, 0u, 0u, 0u}, vr = {0u, 0u, 0u, 0u};
+            uint32_t ke = 0, ve = 0;
+            if (i0 < c) {
+                if (i < c) {
+                    const size_t src = (((size_t)bl * ck.chunk + i) * s.Hkv + kvh) * D + cc * 8;
+                    kr = load16(ck.k_new + src);
+                    vr = load16(ck.v_new + src);
+                }
+                const int page = i < c ? table_page(pg, bl, f + i) : -1;
+                const bool in = page >= 0 && page < pg.n_pages;  // a row without a page is not written
+                const size_t row = pool_row(pg, s.Hkv, kvh, page, f + i);
+                if constexpr (CODES) {
+                    ke = exp_byte<KIND>(group_max<CPR>(amax8(kr)));
+                    ve = exp_byte<KIND>(group_max<CPR>(amax8(vr)));
+                    const u32x2 kc = encode8<KIND>(kr, ke), vc = encode8<KIND>(vr, ve);
+                    kr[0] = kc[0], kr[1] = kc[1], vr[0] = vc[0], vr[1] = vc[1];
+                    if (in) {
+                        *reinterpret_cast<u32x2*>(pg.k + row * D + cc * 8) = kc;
+                        *reinterpret_cast<u32x2*>(pg.v + row * D + cc * 8) = vc;
+                        if (cc == 0) {
+                            pg.k_exp[row] = (uint8_t)ke;
+                            pg.v_exp[row] = (uint8_t)ve;
+                        }
+                    }
+                    odd |= ve == 255u;
+                    if (ve == 255u) ve = 0;  // its values are 0 here
+                } else {
+                    if (in) {
+                        store16(pg.k + (row * D + cc * 8) * 2, kr);
+                        store16(pg.v + (row * D + cc * 8) * 2, vr);
+                    }
+                    odd |= drop_non_finite(vr);
+                }
+            }
+            if constexpr (CODES) {
+                *reinterpret_cast<u32x2*>(kst + B::k_at(i) + cc * 8) = u32x2{kr[0], kr[1]};
+                *reinterpret_cast<u32x2*>(vst + B::v_at(i) + cc * 8) = u32x2{vr[0], vr[1]};
+                if (cc == 0) {
+                    scales[i] = exp_scale(ke);
+                    scales[32 + i] = exp_scale(ve);
+                }
+            } else {
+                store16(kst + B::k_at(i) + cc * 16, kr);
+                store16(vst + B::v_at(i) + cc * 16, vr);
+            }
         }
         asm volatile("" ::: "memory");
-        qr.template step<true>(kst, vst, f, f + c, s.scale2);
-        if (__builtin_amdgcn_ballot_w64(odd) != 0) qr.template add_non_finite<KIND>(s, pg, ck, part, bl, kvh, f, f + c);
+        qr.template step<true>(kst, vst, scales, f, f + c, s.scale2);
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, f, f + c);
         asm volatile("" ::: "memory");
     }
     for (; n0 < t1; n0 += 4 * KB) {
         asm volatile("" ::: "memory");  // this wave's reads of the previous block were issued before
 #pragma unroll
-        for (int it = 0; it < ka.N; ++it) {
-            ka.store(it, lane, kst, kKRow<D>);
-            va.store(it, lane, vst, kVRow<D>);
+        for (int i = 0; i < ka.N; ++i) {
+            store16(kst + B::k_at(ka.row_of(i, lane)) + ka.piece_of(i, lane) * 16, ka.x[i]);
+            store16(vst + B::v_at(ka.row_of(i, lane)) + ka.piece_of(i, lane) * 16, va.x[i]);
         }
+        if constexpr (CODES) scales[lane] = exp_scale(ex);
         if (n0 + 4 * KB < t1) issue(n0 + 4 * KB);
         asm volatile("" ::: "memory");
-        if (n0 + KB <= t1) qr.template step<false>(kst, vst, n0, t1, s.scale2);
-        else qr.template step<true>(kst, vst, n0, t1, s.scale2);
+        if (n0 + KB <= t1) qr.template step<false>(kst, vst, scales, n0, t1, s.scale2);
+        else qr.template step<true>(kst, vst, scales, n0, t1, s.scale2);
     }
     qr.close();
 
@@ -416,6 +621,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = nt * 16 + c16;
+        if (r >= rows) continue;
         if (qq == 0) {
             wm[wave * ROWS + r] = qr.m[nt];
             wl[wave * ROWS + r] = qr.l[nt];
@@ -425,7 +631,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk 
             *reinterpret_cast<f32x4*>(wacc + (size_t)(wave * ROWS + r) * D + 16 * db + 4 * qq) = qr.o[nt][db];
     }
     __syncthreads();
-    float* mine = sp.part + ((size_t)slot * sp.most + split) * ROWS * (D + 2);
+    float* mine = sh.part + (size_t)it.slot(it.share, sh.extras) * ROWS * (D + 2);
     for (int x = tid; x < rows * D; x += kThreads) {
         const int r = x / D, e = x % D;
         float M = kNegInf;
@@ -439,8 +645,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk 
             num += sc * wacc[(size_t)(w * ROWS + r) * D + e];
             den += sc * wl[w * ROWS + r];
         }
-        if (nsplit == 1) {
-            store_out<FINE>(ck, (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + e, num / den);
+        if (it.shares == 1) {
+            store_out<PARTS>(ck, (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + e, num / den);
         } else {
             store_shared(mine + r * (D + 2) + 2 + e, num);
             if (e == 0) {
@@ -449,100 +655,77 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk 
             }
         }
     }
-    if (nsplit == 1) return;
-
-    wait_vmem_ordered();  // this thread's part of the partial has reached memory ...
-    __syncthreads();      // ... and every thread's has, before the mark
-    unsigned long long* marks = sp.marks + (size_t)slot * sp.most;
-    if (tid < 64) {
-        if (tid == 0) __hip_atomic_store(marks + split, sp.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        wait_vmem_ordered();  // the mark has reached memory before the others' are read
-        const bool here = tid >= nsplit ||
-                          __hip_atomic_load(marks + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sp.call;
-        const bool all = __ballot(!here) == 0;
-        if (tid == 0) found = all;
-    }
-    __syncthreads();
-    if (!found) return;
-    const float* base = sp.part + (size_t)slot * sp.most * ROWS * (D + 2);
-    for (int x = tid; x < rows * nsplit; x += kThreads) {  // maxima and sums to LDS
-        const int r = x / nsplit, i = x % nsplit;
-        const float* p = base + ((size_t)i * ROWS + r) * (D + 2);
-        wm[r * kMaxKeySplits + i] = load_shared(p);
-        wm[(ROWS + r) * kMaxKeySplits + i] = load_shared(p + 1);
-    }
-    __syncthreads();
-    for (int x = tid; x < rows * D; x += kThreads) {
-        const int r = x / D, e = x % D;
-        float M = kNegInf;
-        for (int i = 0; i < nsplit; ++i) M = fmaxf(M, wm[r * kMaxKeySplits + i]);
-        const float mu = M == kNegInf ? 0.f : M;
-        float num = 0.f, den = 0.f;
-        for (int i0 = 0; i0 < nsplit; i0 += 8) {
-            float a[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                a[u] = load_shared(base + ((size_t)min(i0 + u, nsplit - 1) * ROWS + r) * (D + 2) + 2 + e);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (i0 + u < nsplit) {
-                    const float sc = fast_exp2(wm[r * kMaxKeySplits + i0 + u] - mu);
-                    num += sc * a[u];
-                    den += sc * wm[(ROWS + r) * kMaxKeySplits + i0 + u];
-                }
-            }
-        }
-        store_out<FINE>(ck, (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + e, num / den);
-    }
-    if (tid < nsplit) __hip_atomic_store(marks + tid, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (it.shares > 1) join_shares<D, ROWS, PARTS>(s, ck, sh, it, rows, 0, wm);
 }
 
-// A workgroup per (segment, KV head, 64 NT query rows).
-template <int D, int KIND, int NT, bool FINE>
-__global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk ck, int tiles) {
+// 16 bytes of a row's staged piece to LDS as bf16: 8 bf16, or 16 codes times their row's power of two.
+template <int KIND>
+__device__ __forceinline__ void put_bf16(char* p, const u32x4& x, float sc) {
+    if constexpr (KIND == kCacheBf16) {
+        store16(p, x);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32x2 a = values4<KIND>(x[2 * h], sc), b = values4<KIND>(x[2 * h + 1], sc);
+            store16(p + 16 * h, u32x4{a[0], a[1], b[0], b[1]});
+        }
+    }
+}
+
+// A workgroup per (segment, KV head, 64 NT query rows), and per share of its keys.
+template <int D, int KIND, int NT, int PARTS>
+__global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk ck, Shares sh, int tiles) {
+    using B = Block<D, false>;
     constexpr int KT = 64;  // keys per tile
-    __shared__ __align__(16) char kst[KT * kKRow<D>];
-    __shared__ __align__(16) char vst[KT * kVRow<D>];
+    constexpr int ROWS = 64 * NT;
+    constexpr int STAGE = KT * (B::K + B::V), JOIN = 2 * ROWS * kMaxShares * (int)sizeof(float);
+    __shared__ __align__(16) char smem[STAGE > JOIN ? STAGE : JOIN];
     __shared__ int odd_seen;
     extern __shared__ uint32_t lds_pages[];
+    char *kst = smem, *vst = smem + KT * B::K;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // the row tiles of a unit follow one another on one XCD (workgroups go to the 8 XCDs in turn), whose L2 then
     // holds the unit's keys
-    const int units = s.B * s.L * s.Hkv;
-    const int x = blockIdx.x / 8, slot = x / tiles * 8 + blockIdx.x % 8, tile = x % tiles;
-    if (slot >= units) return;
-    const int kvh = slot % s.Hkv;
-    const int bl = ck.unit_order != nullptr ? min(max(ck.unit_order[slot / s.Hkv], 0), s.B * s.L - 1) : slot / s.Hkv;
+    const int units = s.B * s.L * s.Hkv, own = (int)blockIdx.x - sh.extras, x8 = own / 8;
+    Item it;
+    if (!take_share(s, pg, ck, sh, tiles, units, x8 / tiles * 8 + (own & 7), x8 % tiles, it)) return;
+    const int bl = it.bl, kvh = it.kvh;
     const Part part = part_of(s, pg, ck, bl);
-    const int rows = part.count * s.G, r_beg = tile * 64 * NT;
+    const int rows = part.count * s.G, r_beg = it.tile * ROWS;
     if (r_beg >= rows) return;
-    const int f = part.first, r_end = min(r_beg + 64 * NT, rows);
-    const int end = f + (r_end - 1) / s.G + 1;  // rows that the workgroup's last token sees
-    const int paged = KIND == kCacheBf16 ? f : end;  // rows read from the pages; the rest from the inputs
+    const int f = part.first, r_end = min(r_beg + ROWS, rows);
+    const int seen = f + (r_end - 1) / s.G + 1;  // rows that the workgroup's last token sees
+    const int t0 = it.shares == 1 ? 0 : min(it.share * it.rows, seen), t1 = it.shares == 1 ? seen : min(t0 + it.rows, seen);
+    const int paged = KIND == kCacheBf16 ? f : seen;  // rows read from the pages; the rest from the inputs
     PageRows pages;
-    pages.init(s, pg, bl, kvh, 0, paged, lds_pages);
+    pages.init(s, pg, bl, kvh, t0, min(t1, paged), lds_pages);
     if (tid == 0) odd_seen = 0;
     __syncthreads();
 
     Staged<D, KIND, KT, kThreads> ka, va;
+    uint32_t ke[ka.N], ve[ka.N];  // codes: the rows' exponent bytes
     auto issue = [&](int n0) {
 #pragma unroll
-        for (int it = 0; it < ka.N; ++it) {
-            const int n = min(n0 + ka.row_of(it, tid), end - 1);
+        for (int i = 0; i < ka.N; ++i) {
+            const int n = min(n0 + ka.row_of(i, tid), t1 - 1);
             if (KIND == kCacheBf16 && n >= f) {
                 const size_t row = ((size_t)bl * ck.chunk + n - f) * s.Hkv + kvh;
-                ka.from_page(it, tid, reinterpret_cast<const uint8_t*>(ck.k_new), nullptr, row);
-                va.from_page(it, tid, reinterpret_cast<const uint8_t*>(ck.v_new), nullptr, row);
+                ka.load(i, tid, reinterpret_cast<const uint8_t*>(ck.k_new), row);
+                va.load(i, tid, reinterpret_cast<const uint8_t*>(ck.v_new), row);
             } else {
                 const size_t row = pages.row(n);
-                ka.from_page(it, tid, pg.k, pg.k_exp, row);
-                va.from_page(it, tid, pg.v, pg.v_exp, row);
+                ka.load(i, tid, pg.k, row);
+                va.load(i, tid, pg.v, row);
+                if constexpr (KIND != kCacheBf16) {
+                    ke[i] = pg.k_exp[row];
+                    ve[i] = pg.v_exp[row];
+                }
             }
         }
     };
-    issue(0);
-    QueryRows<D, NT, FINE> qr;
+    if (t0 < t1) issue(t0);
+    QueryRows<D, NT, PARTS, kCacheBf16> qr;
     const int w0 = r_beg + wave * 16 * NT;  // the wave's first row
     qr.load(s, ck, part, bl, kvh, w0);
     qr.settle_rows();
@@ -550,70 +733,77 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk
     const int all = f + min(w0, rows - 1) / s.G + 1, none = f + min(w0 + 16 * NT - 1, rows - 1) / s.G + 1;
     const bool live = w0 < rows;
 
-    for (int n0 = 0; n0 < end; n0 += KT) {
+    for (int n0 = t0; n0 < t1; n0 += KT) {
         __syncthreads();  // the tile's rows have been read
-        const bool fresh = n0 + KT > f;
-        if (KIND == kCacheBf16 && fresh) {
+        if (n0 + KT > f) {
             bool odd = false;
 #pragma unroll
-            for (int it = 0; it < va.N; ++it) {
-                if (n0 + va.row_of(it, tid) >= f) odd |= drop_non_finite(va.x[it]);
-            }
-            if (odd) odd_seen = 1;
-        }
-        if constexpr (KIND != kCacheBf16) {
-            bool odd = false;
-#pragma unroll
-            for (int it = 0; it < va.N; ++it) {
-                if (n0 + va.row_of(it, tid) >= f && va.e[it] == 255u) {
-                    va.e[it] = 0;
+            for (int i = 0; i < va.N; ++i) {
+                if (n0 + va.row_of(i, tid) < f) continue;
+                if constexpr (KIND == kCacheBf16) {
+                    odd |= drop_non_finite(va.x[i]);
+                } else if (ve[i] == 255u) {
+                    ve[i] = 0;
                     odd = true;
                 }
             }
             if (odd) odd_seen = 1;
         }
 #pragma unroll
-        for (int it = 0; it < ka.N; ++it) {
-            ka.store(it, tid, kst, kKRow<D>);
-            va.store(it, tid, vst, kVRow<D>);
+        for (int i = 0; i < ka.N; ++i) {
+            const int row = ka.row_of(i, tid), at = ka.piece_of(i, tid) * (KIND == kCacheBf16 ? 16 : 32);
+            put_bf16<KIND>(kst + B::k_at(row) + at, ka.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ke[i]));
+            put_bf16<KIND>(vst + B::v_at(row) + at, va.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ve[i]));
         }
-        if (n0 + KT < end) issue(n0 + KT);
+        if (n0 + KT < t1) issue(n0 + KT);
         __syncthreads();
         if (live) {
 #pragma unroll
             for (int b = 0; b < KT; b += 32) {
-                if (n0 + b >= none) continue;
-                if (n0 + b + 32 <= all) qr.template step<false>(kst + b * kKRow<D>, vst + b * kVRow<D>, n0 + b, end, s.scale2);
-                else qr.template step<true>(kst + b * kKRow<D>, vst + b * kVRow<D>, n0 + b, end, s.scale2);
+                if (n0 + b >= min(none, t1)) continue;
+                if (n0 + b + 32 <= min(all, t1)) qr.template step<false>(kst + B::k_at(b), vst + B::v_at(b), nullptr, n0 + b, t1, s.scale2);
+                else qr.template step<true>(kst + B::k_at(b), vst + B::v_at(b), nullptr, n0 + b, t1, s.scale2);
             }
         }
     }
     qr.close();
     __syncthreads();
-    if (odd_seen) qr.template add_non_finite<KIND>(s, pg, ck, part, bl, kvh, f, end);
+    if (odd_seen) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, max(f, t0), t1);
 
     const int c16 = lane & 15, qq = lane >> 4;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = w0 + nt * 16 + c16;
         if (r >= rows) continue;
-        const float inv = 1.f / qr.l[nt];
-        const size_t at = (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + 4 * qq;
+        if (it.shares == 1) {
+            const float inv = 1.f / qr.l[nt];
+            const size_t at = (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + 4 * qq;
 #pragma unroll
-        for (int db = 0; db < D / 16; ++db) {
-            const f32x4 v = qr.o[nt][db] * inv;
-            if constexpr (FINE) {
-                *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(ck.out) + at + 16 * db) = v;
-            } else {
-                const bf16x4 w = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-                *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(ck.out) + at + 16 * db) = w;
+            for (int db = 0; db < D / 16; ++db) {
+                const f32x4 v = qr.o[nt][db] * inv;
+                if constexpr (PARTS > 1) {
+                    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(ck.out) + at + 16 * db) = v;
+                } else {
+                    const bf16x4 w = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+                    *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(ck.out) + at + 16 * db) = w;
+                }
             }
+        } else {
+            float* p = sh.part + ((size_t)it.slot(it.share, sh.extras) * ROWS + r - r_beg) * (D + 2);
+            if (qq == 0) {
+                store_shared(p, qr.m[nt]);
+                store_shared(p + 1, qr.l[nt]);
+            }
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) store_shared(p + 2 + 16 * db + 4 * qq + j, qr.o[nt][db][j]);
         }
     }
     // the new rows into the pages: those of the tokens whose first query row is here
     if constexpr (KIND == kCacheBf16) {
         constexpr int CPR = D / 8;
-        const int i_end = (r_end - 1) / s.G + 1;
+        const int i_end = it.share == 0 ? (r_end - 1) / s.G + 1 : 0;
         for (int i = (r_beg + s.G - 1) / s.G + tid / CPR; i < i_end; i += kThreads / CPR) {
             const int page = table_page(pg, bl, f + i);
             if (page < 0 || page >= pg.n_pages) continue;
@@ -623,41 +813,48 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk
             store16(pg.v + (row * D + e) * 2, load16(ck.v_new + src * D + e));
         }
     }
+    if (it.shares > 1) join_shares<D, ROWS, PARTS>(s, ck, sh, it, r_end - r_beg, r_beg, reinterpret_cast<float*>(smem));
 }
 
-constexpr int kFewRows = 32;  // query rows of a unit up to which few_kernel takes them
+// How a call is dealt out.
+struct Plan {
+    bool few;        // few_kernel
+    int nt, tiles;   // 16-row blocks per wave; row tiles per unit
+    int extras;      // workgroups for the further shares of long items
+    int part_rows;   // query rows of a partial
+};
 
-int few_tiles(const Shape& s, int32_t chunk) { return (int)(((long long)chunk * s.G + 15) / 16); }
-
-// Splits that few_kernel may give a unit's keys.
-int key_splits(const Shape& s, int32_t chunk) {
-    const long long units = (long long)s.B * s.L * s.Hkv;
-    if (units <= 0 || (long long)chunk * s.G > kFewRows) return 1;
-    return (int)std::max<long long>(1, std::min<long long>(2 * kCUs / units, kMaxKeySplits));
+Plan plan_chunk(const Shape& s, int32_t chunk) {
+    const long long units = (long long)s.B * s.L * s.Hkv, rows = (long long)chunk * s.G;
+    Plan p;
+    p.few = rows <= 32;
+    p.nt = p.few ? (rows <= 16 ? 1 : 2) : (rows <= 64 ? 1 : 2);
+    p.tiles = p.few ? 1 : (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
+    p.part_rows = (p.few ? 16 : 64) * p.nt;
+    const long long items = units * p.tiles;
+    p.extras = items > 0 && items <= 2048 && (long long)s.B * s.L <= kScanSegments ? (p.few ? 768 : 512) : 0;
+    return p;
 }
 
-size_t partial_floats(const Shape& s, int32_t chunk, int most) {
-    return most > 1 ? (size_t)s.B * s.L * s.Hkv * most * 16 * few_tiles(s, chunk) * (s.D + 2) : 0;
-}
+size_t partial_floats(const Shape& s, const Plan& p) { return (size_t)2 * p.extras * p.part_rows * (s.D + 2); }
 
-template <int D, int KIND, bool FINE>
+template <int D, int KIND, int PARTS>
 hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
-    const long long units = (long long)s.B * s.L * s.Hkv, rows = (long long)ck.chunk * s.G;
+    const Plan p = plan_chunk(s, ck.chunk);
+    const long long units = (long long)s.B * s.L * s.Hkv;
     const size_t lds = sizeof(uint32_t) * (size_t)pg.max_pages;
-    if (rows <= kFewRows) {
-        KeySplits sp{nullptr, nullptr, 0, key_splits(s, ck.chunk)};
-        if (sp.most > 1) {
-            static std::atomic<unsigned long long> next{
-                (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
-            do sp.call = next.fetch_add(1, std::memory_order_relaxed); while (sp.call == 0);
-            sp.part = ck.ws;
-            sp.marks = reinterpret_cast<unsigned long long*>(ck.ws + partial_floats(s, ck.chunk, sp.most));
-        }
-        const dim3 grid((unsigned)(units * sp.most));
-        if (few_tiles(s, ck.chunk) == 1)
-            hipLaunchKernelGGL((few_kernel<D, KIND, 1, FINE>), grid, dim3(kThreads), lds, st, s, pg, ck, sp);
-        else
-            hipLaunchKernelGGL((few_kernel<D, KIND, 2, FINE>), grid, dim3(kThreads), lds, st, s, pg, ck, sp);
+    Shares sh{nullptr, nullptr, 0, p.extras};
+    if (p.extras > 0) {
+        static std::atomic<unsigned long long> next{
+            (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
+        do sh.call = next.fetch_add(1, std::memory_order_relaxed); while (sh.call == 0);
+        sh.part = ck.ws;
+        sh.marks = reinterpret_cast<unsigned long long*>(ck.ws + partial_floats(s, p));
+    }
+    if (p.few) {
+        const dim3 grid((unsigned)(p.extras + units));
+        if (p.nt == 1) hipLaunchKernelGGL((few_kernel<D, KIND, 1, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh);
+        else hipLaunchKernelGGL((few_kernel<D, KIND, 2, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh);
         return hipGetLastError();
     }
     if constexpr (KIND != kCacheBf16) {
@@ -667,25 +864,26 @@ hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipS
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int nt = rows <= 64 ? 1 : 2;
-    const int tiles = (int)((rows + 64 * nt - 1) / (64 * nt));
-    const dim3 grid((unsigned)((units + 7) / 8 * 8 * tiles));
-    if (nt == 1) hipLaunchKernelGGL((rows_kernel<D, KIND, 1, FINE>), grid, dim3(kThreads), lds, st, s, pg, ck, tiles);
-    else hipLaunchKernelGGL((rows_kernel<D, KIND, 2, FINE>), grid, dim3(kThreads), lds, st, s, pg, ck, tiles);
+    const dim3 grid((unsigned)(p.extras + (units + 7) / 8 * 8 * p.tiles));
+    if (p.nt == 1)
+        hipLaunchKernelGGL((rows_kernel<D, KIND, 1, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh, p.tiles);
+    else
+        hipLaunchKernelGGL((rows_kernel<D, KIND, 2, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh, p.tiles);
     return hipGetLastError();
 }
 
+constexpr int kFineParts = 2;  // bf16 parts of a probability with 32-bit results
+
 template <int D, int KIND>
 hipError_t launch_chunk_k(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
-    return ck.out_bf16 ? launch_chunk_d<D, KIND, false>(s, pg, ck, st) : launch_chunk_d<D, KIND, true>(s, pg, ck, st);
+    return ck.out_bf16 ? launch_chunk_d<D, KIND, 1>(s, pg, ck, st) : launch_chunk_d<D, KIND, kFineParts>(s, pg, ck, st);
 }
 
 }  // namespace
 
 size_t chunk_workspace(const Shape& s, int32_t chunk) {
-    const int most = key_splits(s, chunk);
-    if (most <= 1) return 0;
-    return sizeof(float) * partial_floats(s, chunk, most) + sizeof(unsigned long long) * (size_t)s.B * s.L * s.Hkv * most;
+    const Plan p = plan_chunk(s, chunk);
+    return sizeof(float) * partial_floats(s, p) + sizeof(unsigned long long) * 2 * (size_t)p.extras;
 }
 
 hipError_t launch_chunk(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {

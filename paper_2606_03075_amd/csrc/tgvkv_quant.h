@@ -93,21 +93,17 @@ __device__ __forceinline__ u32x2 encode8(u32x4 r, uint32_t byte) {
 // 4 codes (one register) as 4 bf16 in two registers, without the row's power of two: exact.
 template <int KIND>
 __device__ __forceinline__ u32x2 decode4(uint32_t w) {
-    float f[4];
-    if (KIND == kCacheFp8) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-        f[0] = lo[0];
-        f[1] = lo[1];
-        f[2] = hi[0];
-        f[3] = hi[1];
+    if constexpr (KIND == kCacheFp8) {
+        return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))};
     } else {
+        float f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = (float)(int8_t)(w >> (8 * j));
+        // the upper halves of two floats that are bf16 already
+        return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+                     __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
     }
-    // the upper halves of two floats that are bf16 already
-    return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
-                 __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
 }
 
 // 8 codes as 8 bf16, without the row's power of two.
