@@ -92,21 +92,26 @@ struct Block {
     static constexpr int kBytes = 32 * K, vBytes = 32 * V + (CODES ? 16 : 0);  // of 32 rows
 };
 
-// A lane's 16 bytes of bf16 with what is not finite set to 0; true if there was any.
-__device__ __forceinline__ bool drop_non_finite(u32x4& r) {
-    bool any = false;
+// Whether a lane's 16 bytes of bf16 hold a value that is not finite, and the bytes with such values set to 0.
+__device__ __forceinline__ bool non_finite(const u32x4& r) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 e = {0, 0};  // the larger exponent fields, half by half
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool lo = (r[i] & 0x7F80u) == 0x7F80u, hi = (r[i] & 0x7F800000u) == 0x7F800000u;
-        any |= lo | hi;
-        r[i] = (lo ? 0u : r[i] & 0xFFFFu) | (hi ? 0u : r[i] & 0xFFFF0000u);
-    }
-    return any;
+    for (int i = 0; i < 4; ++i) e = __builtin_elementwise_max(e, __builtin_bit_cast(u16x2, r[i] & 0x7F807F80u));
+    return e[0] == 0x7F80u || e[1] == 0x7F80u;
+}
+__device__ __forceinline__ void drop_non_finite(u32x4& r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        r[i] = ((r[i] & 0x7F80u) == 0x7F80u ? 0u : r[i] & 0xFFFFu) | ((r[i] & 0x7F800000u) == 0x7F800000u ? 0u : r[i] & 0xFFFF0000u);
 }
 
 // 16 NT query rows of one (segment, KV head) in a wave, row 16 nt + l % 16 in lane l.  Keys come as bf16 rows in LDS
 // (CODED = kCacheBf16) or as codes of that kind with their rows' powers of two beside them.  PARTS: bf16 parts of
 // a probability in the product with V.
+// For sched_barrier: vector and scalar arithmetic may cross, matrix and LDS instructions stay in order.
+constexpr int kAluMayCross = 0x2 | 0x4;
+
 template <int D, int NT, int PARTS, int CODED>
 struct QueryRows {
     static constexpr bool CODES = CODED != kCacheBf16;
@@ -145,77 +150,94 @@ struct QueryRows {
             for (int ks = 0; ks < D / 32; ++ks) settle(qf[nt][ks]);
     }
 
-    // One step over the 32 staged rows n0 ..; MASK: only those up to lim count, and below `end`.  scales: with codes,
-    // the rows' powers of two, 32 of K and 32 of V.
-    template <bool MASK>
-    __device__ __forceinline__ void step(const char* kst, const char* vst, const float* scales, int n0, int end, float scale2) {
+    // Logits (unscaled) of 16 NB staged K rows: a[b][nt][j] is row 16 b + 4 (l / 16) + j's.
+    template <int NB>
+    __device__ __forceinline__ void logits(const char* kst, f32x4 (&a)[NB][NT]) const {
         const int c = threadIdx.x & 15, qq = (threadIdx.x & 63) >> 4;
-        f32x4 a[2][NT];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) a[b][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const char *kp0 = kst + B::k_at(c) + qq * 16, *kp1 = kst + B::k_at(16 + c) + qq * 16;
+        const char* kp = kst + B::k_at(c) + qq * 16;
         if constexpr (CODES) {
 #pragma unroll
-            for (int kp = 0; kp < D / 64; ++kp) {
-                const u32x4 w0 = load16(kp0 + kp * 64), w1 = load16(kp1 + kp * 64);
+            for (int k2 = 0; k2 < D / 64; ++k2)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8 k0 = as_bf16x8(decode8<CODED>(u32x2{w0[2 * h], w0[2 * h + 1]}));
-                    const bf16x8 k1 = as_bf16x8(decode8<CODED>(u32x2{w1[2 * h], w1[2 * h + 1]}));
+                for (int b = 0; b < NB; ++b) {
+                    const u32x4 w = load16(kp + B::k_at(16 * b) + k2 * 64);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        a[0][nt] = mfma16x16x32(k0, qf[nt][2 * kp + h], a[0][nt]);
-                        a[1][nt] = mfma16x16x32(k1, qf[nt][2 * kp + h], a[1][nt]);
+                    for (int h = 0; h < 2; ++h) {
+                        const bf16x8 kf = as_bf16x8(decode8<CODED>(u32x2{w[2 * h], w[2 * h + 1]}));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) a[b][nt] = mfma16x16x32(kf, qf[nt][2 * k2 + h], a[b][nt]);
                     }
                 }
-            }
         } else {
+            // the next step's fragments are read before this step's products, and the compiler keeps it so
+            u32x4 kf[2][NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) kf[0][b] = load16(kp + B::k_at(16 * b));
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) {
-                const bf16x8 k0 = as_bf16x8(load16(kp0 + ks * 64)), k1 = as_bf16x8(load16(kp1 + ks * 64));
+                if (ks + 1 < D / 32) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    a[0][nt] = mfma16x16x32(k0, qf[nt][ks], a[0][nt]);
-                    a[1][nt] = mfma16x16x32(k1, qf[nt][ks], a[1][nt]);
+                    for (int b = 0; b < NB; ++b) kf[(ks + 1) & 1][b] = load16(kp + B::k_at(16 * b) + (ks + 1) * 64);
                 }
-            }
-        }
-        f32x4 ksc[2], vsc[2];
-        if constexpr (CODES) {
+                __builtin_amdgcn_sched_barrier(kAluMayCross);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                ksc[b] = *reinterpret_cast<const f32x4*>(scales + 16 * b + 4 * qq);
-                vsc[b] = *reinterpret_cast<const f32x4*>(scales + 32 + 16 * b + 4 * qq);
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) a[b][nt] = mfma16x16x32(as_bf16x8(kf[ks & 1][b]), qf[nt][ks], a[b][nt]);
+                __builtin_amdgcn_sched_barrier(kAluMayCross);
             }
         }
-        bf16x8 pp[PARTS][NT];
+    }
+
+    // MASK: rows n0 + .. above lim, or from `end` on, get -inf.  Then the rows' maxima.  A row's maximum moves only when a
+    // logit is kSlack above it: the probabilities are then at most 2^kSlack, which costs no precision in
+    // floating point, and most steps rescale nothing.
+    template <bool MASK, int NB>
+    __device__ __forceinline__ void raise(f32x4 (&a)[NB][NT], int n0, int end, float scale2) {
+        const int qq = (threadIdx.x & 63) >> 4;
+        constexpr float kSlack = 8.f;
+        float mb[NT];
+        bool grew = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float z[8], mb = kNegInf;
+            mb[nt] = kNegInf;
+            const int last = min(lim[nt], end - 1) - n0 - 4 * qq;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                z[j] = a[j / 4][nt][j % 4];
-                if constexpr (CODES) z[j] *= ksc[j / 4][j % 4];
-                if (MASK) {
-                    const int n = n0 + 16 * (j / 4) + 4 * qq + j % 4;
-                    z[j] = n <= lim[nt] && n < end ? z[j] : kNegInf;
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (MASK) a[b][nt][j] = 16 * b + j <= last ? a[b][nt][j] : kNegInf;
+                    mb[nt] = fmaxf(mb[nt], a[b][nt][j]);
                 }
-                mb = fmaxf(mb, z[j]);
-            }
-            mb = max_xor32(max_xor16(mb)) * scale2;
-            if (__builtin_amdgcn_ballot_w64(mb > m[nt]) != 0) {  // some row's maximum grew (uniform branch)
-                const float mn = fmaxf(m[nt], mb), sc = mn == kNegInf ? 1.f : fast_exp2(m[nt] - mn);
+            mb[nt] = max_xor32(max_xor16(mb[nt])) * scale2;
+            grew |= mb[nt] > m[nt] + kSlack;
+        }
+        if (__builtin_amdgcn_ballot_w64(grew) != 0) {  // uniform branch
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float mn = fmaxf(m[nt], mb[nt]), sc = mn == kNegInf ? 1.f : fast_exp2(m[nt] - mn);
                 l[nt] *= sc;
 #pragma unroll
                 for (int db = 0; db < D / 16; ++db) o[nt][db] *= sc;
                 m[nt] = mn;
             }
+        }
+    }
+
+    // The probabilities of 32 rows (a[0], a[1]) and their product with the staged V rows.  vsc: with codes, the rows' powers of two.
+    __device__ __forceinline__ void weigh(const f32x4* a0, const f32x4* a1, const char* vst, const f32x4* vsc, float scale2) {
+        const int c = threadIdx.x & 15, qq = (threadIdx.x & 63) >> 4;
+        bf16x8 pp[PARTS][NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
             const float mu = m[nt] == kNegInf ? 0.f : m[nt];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float p = fast_exp2(__builtin_fmaf(z[j], scale2, -mu));
+                float p = fast_exp2(__builtin_fmaf(j < 4 ? a0[nt][j % 4] : a1[nt][j % 4], scale2, -mu));
                 l[nt] += p;
                 if constexpr (CODES) p *= vsc[j / 4][j % 4];
                 pp[0][nt][j] = (__bf16)p;
@@ -229,21 +251,66 @@ struct QueryRows {
         // keys of a lane's slots: 4 qq + {0..3}, 16 + 4 qq + {0..3}
         const char* vp = CODES ? vst + B::v_at((c >> 1) < 4 ? 4 * qq + (c >> 1) : 12 + 4 * qq + (c >> 1)) + (c & 1) * 8
                                : vst + B::v_at(4 * qq + (c >> 2)) + (c & 3) * 8;
+        if constexpr (CODES) {
 #pragma unroll
-        for (int db = 0; db < D / 16; ++db) {
-            bf16x8 vv;
-            if constexpr (CODES) {
-                vv = as_bf16x8(decode8<CODED>(__builtin_bit_cast(u32x2, lds_read_tr8(vp + db * 16))));
-            } else {
-                typedef short s16x8 __attribute__((ext_vector_type(8)));
-                const s16x4 v0 = lds_read_tr16(vp + db * 32), v1 = lds_read_tr16(vp + 16 * B::V + db * 32);
-                vv = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+            for (int db = 0; db < D / 16; ++db) {
+                const bf16x8 vv = as_bf16x8(decode8<CODED>(__builtin_bit_cast(u32x2, lds_read_tr8(vp + db * 16))));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < PARTS; ++x) o[nt][db] = mfma16x16x32(vv, pp[x][nt], o[nt][db]);
             }
+        } else {
+            // fragments of two column blocks at a time, read two pairs ahead
+            constexpr int N2 = D / 32;
+            s16x4 vf[3][2][2];
+            auto read = [&](int g) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int d = 0; d < 2; ++d) {
+                    vf[g % 3][d][0] = lds_read_tr16(vp + (2 * g + d) * 32);
+                    vf[g % 3][d][1] = lds_read_tr16(vp + 16 * B::V + (2 * g + d) * 32);
+                }
+            };
+            read(0);
+            read(1);
 #pragma unroll
-                for (int x = 0; x < PARTS; ++x) o[nt][db] = mfma16x16x32(vv, pp[x][nt], o[nt][db]);
+            for (int g = 0; g < N2; ++g) {
+                if (g + 2 < N2) read(g + 2);
+                __builtin_amdgcn_sched_barrier(kAluMayCross);
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x)
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) {
+                        typedef short s16x8 __attribute__((ext_vector_type(8)));
+                        const bf16x8 vv = __builtin_bit_cast(
+                            bf16x8, (s16x8)__builtin_shufflevector(vf[g % 3][d][0], vf[g % 3][d][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) o[nt][2 * g + d] = mfma16x16x32(vv, pp[x][nt], o[nt][2 * g + d]);
+                    }
+                __builtin_amdgcn_sched_barrier(kAluMayCross);
+            }
         }
+    }
+
+    // One step over the 32 staged rows n0 ..  scales: with codes, the rows' powers of two, 32 of K and 32 of V.
+    template <bool MASK>
+    __device__ __forceinline__ void step(const char* kst, const char* vst, const float* scales, int n0, int end, float scale2) {
+        const int qq = (threadIdx.x & 63) >> 4;
+        f32x4 a[2][NT], vsc[2];
+        logits<2>(kst, a);
+        if constexpr (CODES) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 ksc = *reinterpret_cast<const f32x4*>(scales + 16 * b + 4 * qq);
+                vsc[b] = *reinterpret_cast<const f32x4*>(scales + 32 + 16 * b + 4 * qq);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a[b][nt][j] *= ksc[j];
+            }
+        }
+        raise<MASK, 2>(a, n0, end, scale2);
+        weigh(a[0], a[1], vst, vsc, scale2);
     }
 
     // The lane quarters' shares of the sums together.
@@ -492,7 +559,7 @@ __device__ __forceinline__ void join_shares(const Shape& s, const Chunk& ck, con
 }
 
 template <int D, int KIND, int NT, int PARTS>
-__global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk ck, Shares sh) {
+__global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) void few_kernel(Shape s, Pages pg, Chunk ck, Shares sh) {
     constexpr bool CODES = KIND != kCacheBf16;
     using B = Block<D, CODES>;
     constexpr int KB = 32;  // keys per block
@@ -577,7 +644,9 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Shape s, Pages pg, Chunk 
                         store16(pg.k + (row * D + cc * 8) * 2, kr);
                         store16(pg.v + (row * D + cc * 8) * 2, vr);
                     }
-                    odd |= drop_non_finite(vr);
+                    const bool here = non_finite(vr);
+                    odd |= here;
+                    if (__builtin_amdgcn_ballot_w64(here) != 0 && here) drop_non_finite(vr);  // uniform branch
                 }
             }
             if constexpr (CODES) {
@@ -668,22 +737,22 @@ __device__ __forceinline__ void put_bf16(char* p, const u32x4& x, float sc) {
         for (int h = 0; h < 2; ++h) {
             const u32x2 a = values4<KIND>(x[2 * h], sc), b = values4<KIND>(x[2 * h + 1], sc);
             store16(p + 16 * h, u32x4{a[0], a[1], b[0], b[1]});
+            __builtin_amdgcn_sched_barrier(0);  // few values in registers at a time
         }
     }
 }
 
 // A workgroup per (segment, KV head, 64 NT query rows), and per share of its keys.
 template <int D, int KIND, int NT, int PARTS>
-__global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk ck, Shares sh, int tiles) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s, Pages pg, Chunk ck, Shares sh, int tiles) {
     using B = Block<D, false>;
     constexpr int KT = 64;  // keys per tile
     constexpr int ROWS = 64 * NT;
     constexpr int STAGE = KT * (B::K + B::V), JOIN = 2 * ROWS * kMaxShares * (int)sizeof(float);
-    __shared__ __align__(16) char smem[STAGE > JOIN ? STAGE : JOIN];
+    static_assert(STAGE >= JOIN, "room to join the shares");
+    __shared__ __align__(16) char smem[STAGE];
     __shared__ int odd_seen;
     extern __shared__ uint32_t lds_pages[];
-    char *kst = smem, *vst = smem + KT * B::K;
-
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // the row tiles of a unit follow one another on one XCD (workgroups go to the 8 XCDs in turn), whose L2 then
     // holds the unit's keys
@@ -705,23 +774,45 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk
 
     Staged<D, KIND, KT, kThreads> ka, va;
     uint32_t ke[ka.N], ve[ka.N];  // codes: the rows' exponent bytes
+    // Rows behind the last repeat it (they count nothing), so every load is issued.  With bf16 pages new rows come from
+    // the inputs, at a stride of their own: addresses first, by the kind of tile (uniform branches), then the loads.
+    const size_t new_row = (size_t)s.Hkv * D * 2;
+    const size_t new0 = (((size_t)bl * ck.chunk - f) * s.Hkv + kvh) * D * 2;  // row n is at new0 + n new_row
     auto issue = [&](int n0) {
+        const uint8_t *kp[ka.N], *vp[ka.N];
+        if (KIND == kCacheBf16 && n0 >= f) {
 #pragma unroll
-        for (int i = 0; i < ka.N; ++i) {
-            const int n = min(n0 + ka.row_of(i, tid), t1 - 1);
-            if (KIND == kCacheBf16 && n >= f) {
-                const size_t row = ((size_t)bl * ck.chunk + n - f) * s.Hkv + kvh;
-                ka.load(i, tid, reinterpret_cast<const uint8_t*>(ck.k_new), row);
-                va.load(i, tid, reinterpret_cast<const uint8_t*>(ck.v_new), row);
-            } else {
-                const size_t row = pages.row(n);
-                ka.load(i, tid, pg.k, row);
-                va.load(i, tid, pg.v, row);
+            for (int i = 0; i < ka.N; ++i) {
+                const size_t at = new0 + (size_t)min(n0 + ka.row_of(i, tid), t1 - 1) * new_row;
+                kp[i] = reinterpret_cast<const uint8_t*>(ck.k_new) + at;
+                vp[i] = reinterpret_cast<const uint8_t*>(ck.v_new) + at;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < ka.N; ++i) {
+                const size_t row = pages.row(min(n0 + ka.row_of(i, tid), min(t1, paged) - 1));
+                kp[i] = pg.k + row * (D * code_bytes(KIND));
+                vp[i] = pg.v + row * (D * code_bytes(KIND));
                 if constexpr (KIND != kCacheBf16) {
                     ke[i] = pg.k_exp[row];
                     ve[i] = pg.v_exp[row];
                 }
             }
+            if (KIND == kCacheBf16 && n0 + KT > f) {
+#pragma unroll
+                for (int i = 0; i < ka.N; ++i) {
+                    const int n = min(n0 + ka.row_of(i, tid), t1 - 1);
+                    const size_t at = new0 + (size_t)n * new_row;
+                    kp[i] = n >= f ? reinterpret_cast<const uint8_t*>(ck.k_new) + at : kp[i];
+                    vp[i] = n >= f ? reinterpret_cast<const uint8_t*>(ck.v_new) + at : vp[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ka.N; ++i) {
+            // one row tile per unit (NT = 1) reads its keys once; several find them in L2
+            ka.x[i] = load16_global<NT == 1>(kp[i] + ka.piece_of(i, tid) * 16);
+            va.x[i] = load16_global<NT == 1>(vp[i] + ka.piece_of(i, tid) * 16);
         }
     };
     if (t0 < t1) issue(t0);
@@ -729,20 +820,20 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk
     const int w0 = r_beg + wave * 16 * NT;  // the wave's first row
     qr.load(s, ck, part, bl, kvh, w0);
     qr.settle_rows();
-    // the wave's rows see at least the rows below `all`, and none from `none` on
-    const int all = f + min(w0, rows - 1) / s.G + 1, none = f + min(w0 + 16 * NT - 1, rows - 1) / s.G + 1;
-    const bool live = w0 < rows;
+    // the wave's rows see all rows below `all`, and none from `none` on
+    const int all = f + min(w0, rows - 1) / s.G + 1, none = w0 < rows ? f + min(w0 + 16 * NT - 1, rows - 1) / s.G + 1 : 0;
 
-    for (int n0 = t0; n0 < t1; n0 += KT) {
-        __syncthreads();  // the tile's rows have been read
+    // the loaded tile n0 into LDS
+    auto put = [&](int n0, char* st) {
         if (n0 + KT > f) {
             bool odd = false;
 #pragma unroll
             for (int i = 0; i < va.N; ++i) {
-                if (n0 + va.row_of(i, tid) < f) continue;
                 if constexpr (KIND == kCacheBf16) {
-                    odd |= drop_non_finite(va.x[i]);
-                } else if (ve[i] == 255u) {
+                    const bool here = n0 + va.row_of(i, tid) >= f && non_finite(va.x[i]);
+                    odd |= here;
+                    if (__builtin_amdgcn_ballot_w64(here) != 0 && here) drop_non_finite(va.x[i]);  // uniform branch
+                } else if (n0 + va.row_of(i, tid) >= f && ve[i] == 255u) {
                     ve[i] = 0;
                     odd = true;
                 }
@@ -752,19 +843,22 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Shape s, Pages pg, Chunk
 #pragma unroll
         for (int i = 0; i < ka.N; ++i) {
             const int row = ka.row_of(i, tid), at = ka.piece_of(i, tid) * (KIND == kCacheBf16 ? 16 : 32);
-            put_bf16<KIND>(kst + B::k_at(row) + at, ka.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ke[i]));
-            put_bf16<KIND>(vst + B::v_at(row) + at, va.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ve[i]));
+            put_bf16<KIND>(st + B::k_at(row) + at, ka.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ke[i]));
+            put_bf16<KIND>(st + KT * B::K + B::v_at(row) + at, va.x[i], KIND == kCacheBf16 ? 1.f : exp_scale(ve[i]));
         }
+    };
+    for (int n0 = t0; n0 < t1; n0 += KT) {
+        __syncthreads();  // the tile before this one has been read
+        put(n0, smem);
         if (n0 + KT < t1) issue(n0 + KT);
         __syncthreads();
-        if (live) {
-#pragma unroll
-            for (int b = 0; b < KT; b += 32) {
-                if (n0 + b >= min(none, t1)) continue;
-                if (n0 + b + 32 <= min(all, t1)) qr.template step<false>(kst + B::k_at(b), vst + B::v_at(b), nullptr, n0 + b, t1, s.scale2);
-                else qr.template step<true>(kst + B::k_at(b), vst + B::v_at(b), nullptr, n0 + b, t1, s.scale2);
-            }
-        }
+        if (n0 >= none) continue;
+        f32x4 a[4][NT];
+        qr.template logits<4>(smem, a);
+        if (n0 + KT <= min(all, t1)) qr.template raise<false, 4>(a, n0, t1, s.scale2);
+        else qr.template raise<true, 4>(a, n0, t1, s.scale2);
+        qr.weigh(a[0], a[1], smem + KT * B::K, nullptr, s.scale2);
+        qr.weigh(a[2], a[3], smem + KT * B::K + 32 * B::V, nullptr, s.scale2);
     }
     qr.close();
     __syncthreads();

@@ -36,6 +36,14 @@ __device__ __forceinline__ u32x4 load16_stream(const void* p) {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
+// The two loads for an address that the compiler cannot tell to be global memory (chosen among several): it would
+// take a flat load, which counts as an LDS access too.
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load16_global(const void* p) {
+    const auto g = (const __attribute__((address_space(1))) u32x4*)(uintptr_t)p;
+    return STREAM ? __builtin_nontemporal_load(g) : *g;
+}
+
 __device__ __forceinline__ void store16_stream(void* p, u32x4 v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
 }
