@@ -410,12 +410,13 @@ tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts*
  * held so far (budgets plus appended), k_out and v_out are a cache for tgvkv_decode_attn; with count = the new
  * tokens of a chunk and first = the rows before them, they are what the chunk appended.
  * first_or_null int32 [B*L] (null: 0);  count int32 [B*L], clamped to [0, cap];  seg_offsets int64 [B*L+1],
- * ascending.  The rows read must be held: the table row covers them.  Slots count .. cap-1 are left as they
- * are.  k_out, v_out bf16, seg_offsets[B*L] * heads_kv * head_dim elements each. */
+ * ascending.  The rows read must be held; rows that the table row is too narrow to name are not read.  Slots
+ * not read are left as they are.  k_out, v_out bf16, out_rows * heads_kv * head_dim elements each: a segment that
+ * ends behind out_rows is not read, so out_rows >= seg_offsets[B*L] reads all. */
 tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
                               const int32_t* block_table, int32_t max_pages, const int32_t* first_or_null,
-                              const int32_t* count, const int64_t* seg_offsets, void* k_out, void* v_out,
-                              hipStream_t stream);
+                              const int32_t* count, const int64_t* seg_offsets, int64_t out_rows, void* k_out,
+                              void* v_out, hipStream_t stream);
 
 /* tgvkv_chunk_attn_pages -- several new tokens of every sequence over the paged cache: drafted tokens to
  * be checked, the next question, a further image; with chunk 1 a decode step, for pages of any kind.

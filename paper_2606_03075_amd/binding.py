@@ -91,7 +91,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                             vp, vp]
     D = ctypes.POINTER(TgvkvPages)
     lib.tgvkv_compact_pages.argtypes = [P, O, vp, vp, vp, vp, vp, i64, D, vp, i32, vp, vp]
-    lib.tgvkv_read_pages.argtypes = [P, O, D, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.tgvkv_read_pages.argtypes = [P, O, D, vp, i32, vp, vp, vp, i64, vp, vp, vp]
     lib.tgvkv_chunk_attn_pages.argtypes = [P, O, D, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, i32, vp, sz, vp, vp]
     lib.tgvkv_chunk_workspace_size.argtypes = [P, O, i32]
     lib.tgvkv_chunk_workspace_size.restype = sz
@@ -434,10 +434,13 @@ def tgvkv_read_pages(problem, opts, pool, block_table, first, count, seg_offsets
     n = problem.batch * problem.layers
     if first is not None:
         _sized(first, n, "first")
+    if k_out is None or v_out is None or k_out.numel() != v_out.numel():
+        raise ValueError("k_out and v_out must hold the same number of elements")
+    rows = k_out.numel() // (problem.heads_kv * problem.head_dim)
     st = load_library().tgvkv_read_pages(ctypes.byref(problem), _opts_ref(opts), ctypes.byref(_pages(pool, problem)),
                                          _ptr(block_table, _I32, "block_table"), _table_width(block_table, problem),
                                          _ptr(first, _I32, "first"), _ptr(_sized(count, n, "count"), _I32, "count"),
-                                         _ptr(_sized(seg_offsets, n + 1, "seg_offsets"), _I64, "seg_offsets"),
+                                         _ptr(_sized(seg_offsets, n + 1, "seg_offsets"), _I64, "seg_offsets"), rows,
                                          _ptr(k_out, _BF16, "k_out"), _ptr(v_out, _BF16, "v_out"), _stream(stream))
     _check("tgvkv_read_pages", st)
 

@@ -532,21 +532,22 @@ tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts*
 
 tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
                               const int32_t* block_table, int32_t max_pages, const int32_t* first_or_null,
-                              const int32_t* count, const int64_t* seg_offsets, void* k_out, void* v_out,
-                              hipStream_t stream) {
+                              const int32_t* count, const int64_t* seg_offsets, int64_t out_rows, void* k_out,
+                              void* v_out, hipStream_t stream) {
     Shape s;
     tgvkv_status st = make_shape(problem, opts, &s);
     if (st != TGVKV_OK) return st;
     tgvkv::Pages pg;
     st = make_pages(pages, max_pages, block_table, &pg);
     if (st != TGVKV_OK) return st;
-    if (s.B == 0) return TGVKV_OK;
+    if (out_rows < 0) return TGVKV_E_INVAL;
+    if (s.B == 0 || out_rows == 0) return TGVKV_OK;
     if (!pages_present(pg) || count == nullptr || seg_offsets == nullptr || k_out == nullptr || v_out == nullptr)
         return TGVKV_E_INVAL;
     if (!aligned16(k_out) || !aligned16(v_out)) return TGVKV_E_INVAL;
     if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
-    return hip_status(tgvkv::launch_read_pages(s, pg, first_or_null, count, seg_offsets, static_cast<uint16_t*>(k_out),
-                                               static_cast<uint16_t*>(v_out), stream));
+    return hip_status(tgvkv::launch_read_pages(s, pg, first_or_null, count, seg_offsets, out_rows,
+                                               static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), stream));
 }
 
 size_t tgvkv_chunk_workspace_size(const tgvkv_problem* problem, const tgvkv_opts* opts, int32_t chunk) {

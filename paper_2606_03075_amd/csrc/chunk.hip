@@ -348,22 +348,6 @@ struct QueryRows {
     }
 };
 
-// Rows of a segment's pages: the first pool row of every page of rows [n0, n1), in LDS.  A pool's rows are
-// numbered in 32 bits (2^32 of the smallest rows, in two pools, are more memory than the GPU has).
-struct PageRows {
-    const uint32_t* base;
-    int p0, shift;
-    __device__ __forceinline__ void init(const Shape& s, const Pages& pg, int bl, int kvh, int n0, int n1, uint32_t* lds) {
-        shift = pg.shift;
-        p0 = n0 >> shift;
-        base = lds;
-        const int p1 = n1 > n0 ? ((n1 - 1) >> shift) + 1 : p0;
-        for (int i = p0 + (int)threadIdx.x; i < p1; i += kThreads)
-            lds[i - p0] = (uint32_t)pool_row(pg, s.Hkv, kvh, pg.table[(size_t)bl * pg.max_pages + i], 0);
-    }
-    __device__ __forceinline__ size_t row(int n) const { return base[(n >> shift) - p0] + (uint32_t)(n & ((1 << shift) - 1)); }
-};
-
 // One lane's share of `ROWS` rows' K or V on its way from the pages.  LANES lanes work together, each on 16
 // bytes of a row at a time: 8 bf16, or 16 codes.
 template <int D, int KIND, int ROWS, int LANES>
@@ -581,7 +565,7 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
     const bool last_share = it.share == it.shares - 1;  // takes the new rows
     const int t0 = min(it.share * it.rows, f), t1 = it.shares == 1 ? f : min(t0 + it.rows, f);
     PageRows pages;
-    pages.init(s, pg, bl, kvh, t0, t1, lds_pages);
+    pages.init<kThreads>(s, pg, bl, kvh, t0, t1, lds_pages);
     __syncthreads();
 
     char* kst = smem + wave * STAGE;
@@ -735,8 +719,7 @@ __device__ __forceinline__ void put_bf16(char* p, const u32x4& x, float sc) {
     } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const u32x2 a = values4<KIND>(x[2 * h], sc), b = values4<KIND>(x[2 * h + 1], sc);
-            store16(p + 16 * h, u32x4{a[0], a[1], b[0], b[1]});
+            store16(p + 16 * h, values8<KIND>(u32x2{x[2 * h], x[2 * h + 1]}, sc));
             __builtin_amdgcn_sched_barrier(0);  // few values in registers at a time
         }
     }
@@ -768,7 +751,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
     const int t0 = it.shares == 1 ? 0 : min(it.share * it.rows, seen), t1 = it.shares == 1 ? seen : min(t0 + it.rows, seen);
     const int paged = KIND == kCacheBf16 ? f : seen;  // rows read from the pages; the rest from the inputs
     PageRows pages;
-    pages.init(s, pg, bl, kvh, t0, min(t1, paged), lds_pages);
+    pages.init<kThreads>(s, pg, bl, kvh, t0, min(t1, paged), lds_pages);
     if (tid == 0) odd_seen = 0;
     __syncthreads();
 
@@ -936,7 +919,7 @@ template <int D, int KIND, int PARTS>
 hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
     const Plan p = plan_chunk(s, ck.chunk);
     const long long units = (long long)s.B * s.L * s.Hkv;
-    const size_t lds = sizeof(uint32_t) * (size_t)pg.max_pages;
+    const size_t lds = lds_pages_bytes(pg);
     Shares sh{nullptr, nullptr, 0, p.extras};
     if (p.extras > 0) {
         static std::atomic<unsigned long long> next{

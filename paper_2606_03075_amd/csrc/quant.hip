@@ -1,11 +1,14 @@
 // The paged cache in 8 bits: the retained rows quantised as they are written, and rows read back.
 //
 // Both are HBM streams.  compact_pages_kernel is compact_kernel with a different store: a row of head_dim
-// bf16 is read by head_dim/8 lanes with 16-byte loads, the lanes agree on its largest magnitude by row
-// swaps on the vector units, and each writes 8 codes; the row's first lane writes its exponent byte.
-// read_pages_kernel goes the other way, from pages of any kind to contiguous bf16 rows.
+// bf16 is read by head_dim/8 lanes with 16-byte loads, the lanes agree on its largest magnitude by lane swaps
+// on the vector units, and each writes 8 codes; the row's first lane writes its exponent byte.
+// read_pages_kernel goes the other way, from pages of any kind to contiguous bf16 rows.  Each thread keeps
+// kPasses rows' K and V in flight (one row at a time was bound by latency: 298 us to store and 384 us to read
+// 1.2 M rows of 128, layers of 30 to 2979 rows), and page ids are looked up in LDS.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "tgvkv_quant.h"
 #include "tgvkv_shape.h"
@@ -14,6 +17,8 @@ namespace tgvkv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kPasses = 8;
+constexpr int kMaxRowGroups = 16384;
 
 template <int D, int KIND>
 __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages pg, const uint16_t* __restrict__ k,
@@ -22,8 +27,9 @@ __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages 
                                                                  const int32_t* __restrict__ budgets,
                                                                  const int64_t* __restrict__ idx_off, int nsplit,
                                                                  const int32_t* __restrict__ unit_order) {
-    constexpr int CPR = D / 8;
-    constexpr int RPP = kThreads / CPR;
+    extern __shared__ uint32_t lds_pages[];
+    constexpr int CPR = D / 8;           // lanes per row
+    constexpr int RPP = kThreads / CPR;  // rows per pass
     int bid = blockIdx.x;
     const int split = bid % nsplit;
     bid /= nsplit;
@@ -31,21 +37,45 @@ __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages 
     const int bl = unit_order != nullptr ? min(max(unit_order[bid / s.Hkv], 0), s.B * s.L - 1) : bid / s.Hkv;
     const int bsz = budgets[bl];
     const long long ioff = idx_off[bl] + (s.head_mode == 0 ? 0 : (long long)kvh * bsz);
-    const int per = (bsz + nsplit - 1) / nsplit;
-    const int r_beg = min(split * per, bsz), r_end = min(r_beg + per, bsz);
+    const int held = (int)min((long long)bsz, (long long)pg.max_pages << pg.shift);  // rows that the table can name
+    const int per = (held + nsplit - 1) / nsplit;
+    const int r_beg = min(split * per, held), r_end = min(r_beg + per, held);
+    if (r_beg >= r_end) return;  // uniform, before any barrier
     const int cc = threadIdx.x % CPR, rl = threadIdx.x / CPR;
     const size_t src0 = ((size_t)bl * s.Hkv + kvh) * (size_t)s.N * D + cc * 8;
-    // the lanes of a row take the same branch, so the row's maximum is taken among active lanes
-    for (int r = r_beg + rl; r < r_end; r += RPP) {
-        const int pos = min(max(idx[ioff + r], 0), s.N - 1);
-        const u32x4 kr = load16_stream(k + src0 + (size_t)pos * D), vr = load16_stream(v + src0 + (size_t)pos * D);
-        const size_t row = pool_row(pg, s.Hkv, kvh, table_page(pg, bl, r), r);
-        const uint32_t ke = exp_byte<KIND>(group_max<CPR>(amax8(kr))), ve = exp_byte<KIND>(group_max<CPR>(amax8(vr)));
-        *reinterpret_cast<u32x2*>(pg.k + row * D + cc * 8) = encode8<KIND>(kr, ke);
-        *reinterpret_cast<u32x2*>(pg.v + row * D + cc * 8) = encode8<KIND>(vr, ve);
-        if (cc == 0) {
-            pg.k_exp[row] = (uint8_t)ke;
-            pg.v_exp[row] = (uint8_t)ve;
+    // positions come from tgvkv_select; clamped so a corrupt index can never read outside the slice.  Rows behind the
+    // last repeat it and are not stored.
+    int pos[kPasses];
+    auto positions = [&](int r0) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) pos[i] = min(max(idx[ioff + min(r0 + i * RPP + rl, r_end - 1)], 0), s.N - 1);
+    };
+    positions(r_beg);
+    PageRows pages;
+    pages.init<kThreads>(s, pg, bl, kvh, r_beg, r_end, lds_pages);
+    __syncthreads();
+    for (int r0 = r_beg; r0 < r_end; r0 += RPP * kPasses) {
+        u32x4 kr[kPasses], vr[kPasses];
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            kr[i] = load16_stream(k + src0 + (size_t)pos[i] * D);
+            vr[i] = load16_stream(v + src0 + (size_t)pos[i] * D);
+        }
+        positions(r0 + RPP * kPasses);
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int r = r0 + i * RPP + rl;
+            // every lane takes part in the row's maximum
+            const uint32_t ke = exp_byte<KIND>(group_max<CPR>(amax8(kr[i]))), ve = exp_byte<KIND>(group_max<CPR>(amax8(vr[i])));
+            if (r < r_end) {
+                const size_t row = pages.row(r);
+                *reinterpret_cast<u32x2*>(pg.k + row * D + cc * 8) = encode8<KIND>(kr[i], ke);
+                *reinterpret_cast<u32x2*>(pg.v + row * D + cc * 8) = encode8<KIND>(vr[i], ve);
+                if (cc == 0) {
+                    pg.k_exp[row] = (uint8_t)ke;
+                    pg.v_exp[row] = (uint8_t)ve;
+                }
+            }
         }
     }
 }
@@ -53,8 +83,9 @@ __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages 
 template <int D, int KIND>
 __global__ __launch_bounds__(kThreads) void read_pages_kernel(Shape s, Pages pg, const int32_t* __restrict__ first,
                                                               const int32_t* __restrict__ count,
-                                                              const int64_t* __restrict__ seg_off, int nsplit,
-                                                              uint16_t* __restrict__ kc, uint16_t* __restrict__ vc) {
+                                                              const int64_t* __restrict__ seg_off, int64_t out_rows,
+                                                              int nsplit, uint16_t* __restrict__ kc, uint16_t* __restrict__ vc) {
+    extern __shared__ uint32_t lds_pages[];
     constexpr int CPR = D / 8;
     constexpr int RPP = kThreads / CPR;
     int bid = blockIdx.x;
@@ -62,41 +93,60 @@ __global__ __launch_bounds__(kThreads) void read_pages_kernel(Shape s, Pages pg,
     bid /= nsplit;
     const int kvh = bid % s.Hkv, bl = bid / s.Hkv;
     const int64_t s0 = seg_off[bl], cap = seg_off[bl + 1] - s0;
+    if (s0 < 0 || cap < 0 || s0 + cap > out_rows) return;  // a segment that the output does not hold
     const int f = first != nullptr ? max(first[bl], 0) : 0;
-    const int rows = (int)min((int64_t)max(count[bl], 0), cap);
+    // rows that the table can name
+    const long long most = ((long long)pg.max_pages << pg.shift) - f;
+    const int rows = (int)max(min(min((long long)max(count[bl], 0), (long long)cap), most), 0ll);
     const int per = (rows + nsplit - 1) / nsplit;
     const int r_beg = min(split * per, rows), r_end = min(r_beg + per, rows);
+    if (r_beg >= r_end) return;  // uniform, before any barrier
     const int cc = threadIdx.x % CPR, rl = threadIdx.x / CPR;
+    PageRows pages;
+    pages.init<kThreads>(s, pg, bl, kvh, f + r_beg, f + r_end, lds_pages);
+    __syncthreads();
     const size_t dst0 = ((size_t)s0 * s.Hkv + (size_t)kvh * cap) * D + cc * 8;
-    for (int r = r_beg + rl; r < r_end; r += RPP) {
-        const size_t row = pool_row(pg, s.Hkv, kvh, table_page(pg, bl, f + r), f + r);
-        const size_t at = (row * D + cc * 8) * code_bytes(KIND);
-        u32x4 kr, vr;
-        if constexpr (KIND == kCacheBf16) {
-            kr = load16_stream(pg.k + at);
-            vr = load16_stream(pg.v + at);
-        } else {
-            kr = decode8<KIND>(*reinterpret_cast<const u32x2*>(pg.k + at));
-            vr = decode8<KIND>(*reinterpret_cast<const u32x2*>(pg.v + at));
-            const float ks = exp_scale(pg.k_exp[row]), vs = exp_scale(pg.v_exp[row]);
+    auto move = [&](auto passes, int r0) {
+        constexpr int N = decltype(passes)::value;
+        u32x4 kr[N], vr[N];
+        uint32_t ke[N], ve[N];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                kr[i] = scale2bf16(kr[i], ks);
-                vr[i] = scale2bf16(vr[i], vs);
+        for (int i = 0; i < N; ++i) {  // rows behind the last repeat it and are not stored
+            const size_t row = pages.row(f + min(r0 + i * RPP + rl, r_end - 1)), at = (row * D + cc * 8) * code_bytes(KIND);
+            if constexpr (KIND == kCacheBf16) {
+                kr[i] = load16_stream(pg.k + at);
+                vr[i] = load16_stream(pg.v + at);
+            } else {
+                const u32x2 kc8 = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(pg.k + at));
+                const u32x2 vc8 = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(pg.v + at));
+                kr[i][0] = kc8[0], kr[i][1] = kc8[1], vr[i][0] = vc8[0], vr[i][1] = vc8[1];
+                ke[i] = pg.k_exp[row];
+                ve[i] = pg.v_exp[row];
             }
         }
-        store16(kc + dst0 + (size_t)r * D, kr);
-        store16(vc + dst0 + (size_t)r * D, vr);
-    }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = r0 + i * RPP + rl;
+            if (r >= r_end) continue;
+            if constexpr (KIND != kCacheBf16) {
+                kr[i] = values8<KIND>(u32x2{kr[i][0], kr[i][1]}, exp_scale(ke[i]));
+                vr[i] = values8<KIND>(u32x2{vr[i][0], vr[i][1]}, exp_scale(ve[i]));
+            }
+            store16(kc + dst0 + (size_t)r * D, kr[i]);
+            store16(vc + dst0 + (size_t)r * D, vr[i]);
+        }
+    };
+    int r0 = r_beg;
+    for (; r_end - r0 > RPP; r0 += RPP * kPasses) move(std::integral_constant<int, kPasses>(), r0);
+    if (r0 < r_end) move(std::integral_constant<int, 1>(), r0);  // a chunk's few rows, or the last ones
 }
 
-// Workgroups per (sequence, layer, KV head), as compaction's.
+// Workgroups per (sequence, layer, KV head): about one per 64 rows of the mean segment.  Segments differ in
+// length by an order of magnitude, and small shares even that out (1.2 M rows in 4096 units of 30 to 2979: 200 us
+// with 4 each, 300 with one), but workgroups without rows are not free: 16384 of them take 40 us.
 int row_splits(const Shape& s, int64_t rows_total) {
-    const long long units = (long long)s.B * s.L * s.Hkv;
-    if (units <= 0 || rows_total <= 0) return 1;
-    const long long avg_rows = rows_total / ((long long)s.B * s.L);
-    const long long n = std::min<long long>(2048 / units, avg_rows / 64);
-    return (int)std::max<long long>(1, std::min<long long>(n, 16));
+    const long long units = (long long)s.B * s.L * s.Hkv, mean = rows_total / std::max<long long>((long long)s.B * s.L, 1);
+    return (int)std::max<long long>(1, std::min<long long>({kMaxRowGroups / std::max<long long>(units, 1), mean / 64, 16}));
 }
 
 }  // namespace
@@ -108,7 +158,7 @@ hipError_t launch_compact_pages(const Shape& s, const Pages& pg, const uint16_t*
     const int nsplit = row_splits(s, rows_total);
     const dim3 grid((unsigned)((long long)s.B * s.L * s.Hkv * nsplit));
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, s, pg, k, v, idx, budgets, idx_off, nsplit, unit_order);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds_pages_bytes(pg), st, s, pg, k, v, idx, budgets, idx_off, nsplit, unit_order);
     };
     if (pg.kind == kCacheFp8) {
         if (s.D == 128) launch(compact_pages_kernel<128, kCacheFp8>);
@@ -121,13 +171,12 @@ hipError_t launch_compact_pages(const Shape& s, const Pages& pg, const uint16_t*
 }
 
 hipError_t launch_read_pages(const Shape& s, const Pages& pg, const int32_t* first, const int32_t* count,
-                             const int64_t* seg_off, uint16_t* kc, uint16_t* vc, hipStream_t st) {
-    if (s.B * s.L == 0) return hipSuccess;
-    const long long units = (long long)s.B * s.L * s.Hkv;
-    const int nsplit = (int)std::max<long long>(1, std::min<long long>(2048 / units, 16));
-    const dim3 grid((unsigned)(units * nsplit));
+                             const int64_t* seg_off, int64_t out_rows, uint16_t* kc, uint16_t* vc, hipStream_t st) {
+    if (out_rows <= 0 || s.B * s.L == 0) return hipSuccess;
+    const int nsplit = row_splits(s, out_rows);
+    const dim3 grid((unsigned)((long long)s.B * s.L * s.Hkv * nsplit));
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, s, pg, first, count, seg_off, nsplit, kc, vc);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds_pages_bytes(pg), st, s, pg, first, count, seg_off, out_rows, nsplit, kc, vc);
     };
     if (s.D == 128) {
         if (pg.kind == kCacheBf16) launch(read_pages_kernel<128, kCacheBf16>);

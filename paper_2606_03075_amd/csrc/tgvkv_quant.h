@@ -113,29 +113,25 @@ __device__ __forceinline__ u32x4 decode8(u32x2 c) {
     return u32x4{a[0], a[1], b[0], b[1]};
 }
 
-// 4 codes as the 4 bf16 that they stand for, s = 2^e of their row (byte 255: s is inf, 0 * inf = NaN).
+// 8 codes as the 8 bf16 that they stand for, s = 2^e of their row: exact.  (Byte 255: s is inf and the values NaN, by
+// 0 * inf, or by the conversion's own rule for that exponent.)
 template <int KIND>
-__device__ __forceinline__ u32x2 values4(uint32_t w, float s) {
-    float f[4];
-    if (KIND == kCacheFp8) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-        f[0] = lo[0] * s;
-        f[1] = lo[1] * s;
-        f[2] = hi[0] * s;
-        f[3] = hi[1] * s;
-    } else {
+__device__ __forceinline__ u32x4 values8(u32x2 c, float s) {
+    u32x4 r;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j] = (float)(int8_t)(w >> (8 * j)) * s;
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (KIND == kCacheFp8) {
+            r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, false));
+            r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, true));
+        } else {
+            float f[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = (float)(int8_t)(c[i] >> (8 * j)) * s;
+            r[2 * i] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+            r[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+        }
     }
-    return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
-                 __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
-}
-
-// 2 bf16 times a power of two, as bf16 (exact in the normal range; inf * 0 = NaN for the byte 255).
-__device__ __forceinline__ uint32_t scale2bf16(uint32_t w, float s) {
-    return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(w & 0xFFFF0000u) * s),
-                                 __float_as_uint(__uint_as_float(w << 16) * s), 0x07060302u);
+    return r;
 }
 
 // Row `n` of segment bl: the pool's row index of KV head kvh (an id outside the pool is clamped into it).
@@ -146,5 +142,24 @@ __device__ __forceinline__ size_t pool_row(const Pages& pg, int hkv, int kvh, in
 __device__ __forceinline__ int table_page(const Pages& pg, int bl, int n) {
     return pg.table[(size_t)bl * pg.max_pages + min(n >> pg.shift, pg.max_pages - 1)];
 }
+
+// Rows of a segment's pages: the first pool row of every page of rows [n0, n1), in LDS.  A pool's rows are
+// numbered in 32 bits (2^32 of the smallest rows, in two pools, are more memory than the GPU has).
+struct PageRows {
+    const uint32_t* base;
+    int p0, shift;
+    template <int THREADS>
+    __device__ __forceinline__ void init(const Shape& s, const Pages& pg, int bl, int kvh, int n0, int n1, uint32_t* lds) {
+        shift = pg.shift;
+        p0 = n0 >> shift;
+        base = lds;
+        const int p1 = n1 > n0 ? ((n1 - 1) >> shift) + 1 : p0;
+        for (int i = p0 + (int)threadIdx.x; i < p1; i += THREADS)
+            lds[i - p0] = (uint32_t)pool_row(pg, s.Hkv, kvh, pg.table[(size_t)bl * pg.max_pages + i], 0);
+    }
+    __device__ __forceinline__ size_t row(int n) const { return base[(n >> shift) - p0] + (uint32_t)(n & ((1 << shift) - 1)); }
+};
+
+inline size_t lds_pages_bytes(const Pages& pg) { return sizeof(uint32_t) * (size_t)pg.max_pages; }
 
 }  // namespace tgvkv

@@ -113,7 +113,7 @@ hipError_t launch_compact_pages(const Shape& s, const Pages& pg, const uint16_t*
                                 const int32_t* idx, const int32_t* budgets, const int64_t* idx_off, int64_t rows_total,
                                 const int32_t* unit_order, hipStream_t st);
 hipError_t launch_read_pages(const Shape& s, const Pages& pg, const int32_t* first, const int32_t* count,
-                             const int64_t* seg_off, uint16_t* kc, uint16_t* vc, hipStream_t st);
+                             const int64_t* seg_off, int64_t out_rows, uint16_t* kc, uint16_t* vc, hipStream_t st);
 
 // A call's new tokens: up to `chunk` per sequence, n_new[b] of them (null: all), from step steps[b] on.
 struct Chunk {

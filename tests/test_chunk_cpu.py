@@ -75,8 +75,8 @@ def test_store_and_read_refusals(so):
         return so.tgvkv_compact_pages(ctypes.byref(problem or P()), None, k, v, idx, budgets, offs, total, pool, table, width,
                                       None, S)
 
-    def read(problem=None, pool=pages(), table=FAKE, width=2, count=FAKE, seg=FAKE, k=FAKE, v=FAKE):
-        return so.tgvkv_read_pages(ctypes.byref(problem or P()), None, pool, table, width, None, count, seg, k, v, S)
+    def read(problem=None, pool=pages(), table=FAKE, width=2, count=FAKE, seg=FAKE, rows=9, k=FAKE, v=FAKE):
+        return so.tgvkv_read_pages(ctypes.byref(problem or P()), None, pool, table, width, None, count, seg, rows, k, v, S)
     for bad, code in BAD_POOLS:
         assert store(pool=pages(**bad)) == code, bad
         assert read(pool=pages(**bad)) == code, bad
@@ -87,8 +87,9 @@ def test_store_and_read_refusals(so):
         assert store(**bad) == code, bad
         assert store(pool=pages(kind=0), **bad) == code, bad  # as tgvkv_compact_paged
     for bad, code in [(dict(table=None), -1), (dict(width=0), -1), (dict(width=4097), -2), (dict(count=None), -1),
-                      (dict(seg=None), -1), (dict(k=None), -1), (dict(v=ODD), -1), (dict(problem=P(head_dim=32)), -2)]:
+                      (dict(seg=None), -1), (dict(rows=-1), -1), (dict(k=None), -1), (dict(v=ODD), -1), (dict(problem=P(head_dim=32)), -2)]:
         assert read(**bad) == code, bad
+    assert read(rows=0, k=None) == 0
     assert store(problem=P(batch=0), pool=pages(k=None)) == read(problem=P(batch=0), pool=pages(k=None)) == 0
 
 

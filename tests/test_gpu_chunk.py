@@ -114,6 +114,27 @@ def test_later_tokens_do_not_show(lib, kind, chunk, where, value):
         assert np.all(np.isnan(got) | (got == value)) and np.any(got == value)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("chunk", [2, 70])
+@pytest.mark.parametrize("where", [0, 1])
+def test_bad_retained_rows(lib, kind, chunk, where):
+    """A NaN in a retained key makes every result of its segment NaN; in a retained value, that dim's, or with 8-bit
+    rows every dim's.  The other segment is as it was."""
+    log(f"chunk bad retained row kind={kind} chunk={chunk} where={where}")
+    c = case(16, 2, 1, 6, 2, 128, chunk, kind, 16, [50, 33], [0, 1], None, chunk + 1)
+    from tests.pages_util import bits
+    row = bits(np.ones((2, 128)))
+    row[:, 9] = 0x7FC0
+    c["pool"].write(where, c["table"][0], 20, row)
+    out, _ = call(c)
+    dims = [9] if where == 1 and kind == bd.CACHE_BF16 else list(range(128))
+    assert np.all(np.isnan(out[0][..., dims]))
+    if len(dims) == 1:
+        assert np.all(np.isfinite(np.delete(out[0], 9, axis=-1)))
+    want, mag, qk = reference(c)
+    assert np.all((np.abs(out - want) <= tolerance(c, want, mag, qk, False))[1])
+
+
 def test_extreme_logits(lib):
     """Logits far apart (one key takes all), equal, and so low that a key of probability 0 has a value of 1e38."""
     from tests.pages_util import bits

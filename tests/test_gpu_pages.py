@@ -176,6 +176,32 @@ def test_read_parts(lib, kind):
         assert np.array_equal(np.where(got == 0x8000, 0, got), np.where(want == 0x8000, 0, want))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_read_stays_in_the_output(lib, kind):
+    """A segment that ends behind the output is left out, the others are read; nor is anything behind the table's rows."""
+    import torch
+    log(f"read bounds kind={kind}")
+    rng = np.random.default_rng(6)
+    ref = Pool(6, 2, 8, 64, kind)
+    table = np.array([[3, 1], [0, 4], [5, 2]], np.int32)
+    for w in range(2):
+        for i in range(3):
+            for r in range(16):
+                ref.write(w, table[i], r, bits(rng.standard_normal((2, 64))))
+    p = bd.make_problem(3, 1, 2, 2, 64, 1, 0, 0)
+    so = np.array([0, 10, 40, 52], np.int64)
+    out = [torch.full((45 * 2 * 64,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ref.device().read(p, None, _up(table), _up(np.array([10, 30, 5], np.int32)), _up(so), *out,
+                      first=_up(np.array([2, 4, 0], np.int32)))
+    torch.cuda.synchronize()
+    for w, got in enumerate(out):
+        want = np.full(got.numel(), bits(7.0), np.uint16)
+        want[:10 * 128].reshape(2, 10, 64)[:] = bits(ref.rows(w, table[0], 2, 12))
+        want[10 * 128:40 * 128].reshape(2, 30, 64)[:, :12] = bits(ref.rows(w, table[1], 4, 16))
+        got = bf16_host_bits(got)
+        assert np.array_equal(np.where(got == 0x8000, 0, got), np.where(want == 0x8000, 0, want))
+
+
 @pytest.mark.parametrize("kind", Q8)
 def test_bad_rows_read_as_nan(lib, kind):
     """A retained row with an infinity reads as NaN in every place, its neighbours do not."""
