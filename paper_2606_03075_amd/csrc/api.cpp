@@ -577,7 +577,8 @@ tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_op
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out)) return TGVKV_E_INVAL;
     const size_t need = align_up(tgvkv::chunk_workspace(s, chunk));
     if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return TGVKV_E_WORKSPACE;
-    const tgvkv::Chunk ck{budgets, steps, n_new_or_null, decode_reserve, chunk, static_cast<const uint16_t*>(q),
+    const uint32_t inv_g = (uint32_t)(((uint64_t(1) << 32) + s.G - 1) / s.G);
+    const tgvkv::Chunk ck{budgets, steps, n_new_or_null, decode_reserve, chunk, inv_g, static_cast<const uint16_t*>(q),
                           static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), out, out_bf16,
                           unit_order_or_null, static_cast<float*>(workspace)};
     return hip_status(tgvkv::launch_chunk(s, pg, ck, stream));

@@ -53,6 +53,16 @@ __device__ __forceinline__ Part part_of(const Shape& s, const Pages& pg, const C
     return ok ? Part{bsz + st, c} : Part{0, 0};
 }
 
+// Token and head of query row r = i G + g: r / G by a multiplication (exact below 2^28, and a segment's rows end at 2^24).
+__device__ __forceinline__ int token_of(const Shape& s, const Chunk& ck, int r) {
+    return s.G == 1 ? r : (int)__umulhi((unsigned)r, ck.inv_g);
+}
+// First element of query row r in q and out.
+__device__ __forceinline__ size_t query_at(const Shape& s, const Chunk& ck, int bl, int kvh, int r, int D) {
+    const int i = token_of(s, ck, r);
+    return (((size_t)bl * ck.chunk + i) * s.H + kvh * s.G + (r - i * s.G)) * D;
+}
+
 // The new rows into the pages, for rows_kernel on 8-bit pages (its many row tiles then read codes).
 template <int D, int KIND>
 __global__ __launch_bounds__(kThreads) void append_kernel(Shape s, Pages pg, Chunk ck) {
@@ -131,12 +141,11 @@ struct QueryRows {
         for (int nt = 0; nt < NT; ++nt) {
             const int r = r0 + nt * 16 + c, rows = part.count * s.G;
             const bool in = r < rows;
-            const int i = min(r, rows - 1) / s.G, g = min(r, rows - 1) % s.G;
-            const uint16_t* qp = ck.q + (((size_t)bl * ck.chunk + i) * s.H + kvh * s.G + g) * D;
+            const uint16_t* qp = ck.q + query_at(s, ck, bl, kvh, min(r, rows - 1), D);
             const u32x4 z = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) qf[nt][ks] = as_bf16x8(in ? load16(qp + dim_of(ks, qq)) : z);
-            lim[nt] = part.first + i;
+            lim[nt] = part.first + token_of(s, ck, min(r, rows - 1));
             m[nt] = kNegInf;
             l[nt] = 0.f;
 #pragma unroll
@@ -357,9 +366,6 @@ struct Staged {
     u32x4 x[N];
     __device__ __forceinline__ static int row_of(int it, int lane) { return (it * LANES + lane) / CH; }
     __device__ __forceinline__ static int piece_of(int it, int lane) { return (it * LANES + lane) % CH; }
-    __device__ __forceinline__ void load(int it, int lane, const uint8_t* pool, size_t row) {
-        x[it] = load16_stream(pool + (row * CH + piece_of(it, lane)) * 16);
-    }
 };
 
 // Results of a row: f32 or bf16.
@@ -535,8 +541,7 @@ __device__ __forceinline__ void join_shares(const Shape& s, const Chunk& ck, con
                 den += sc * ml[(ROWS + r) * kMaxShares + i];
             }
         }
-        const int q = r0 + r;
-        store_out<PARTS>(ck, (((size_t)it.bl * ck.chunk + q / s.G) * s.H + it.kvh * s.G + q % s.G) * D + e, num / den);
+        store_out<PARTS>(ck, query_at(s, ck, it.bl, it.kvh, r0 + r, D) + e, num / den);
     }
     if (tid < n)
         __hip_atomic_store(sh.marks + it.slot(tid, sh.extras), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -573,13 +578,27 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
     float* scales = reinterpret_cast<float*>(kst + (B::kBytes + B::vBytes + 15) / 16 * 16);
     Staged<D, KIND, KB, 64> ka, va;
     uint32_t ex = 0;  // codes: exponent byte of K row `lane`, or of V row `lane` - 32
-    // rows behind the last repeat it (they count nothing), so every load is issued
+    // A load instruction of the wave takes RPI rows.  Where they are one page's, their address is one scalar (the lanes'
+    // own offsets never change); else, and at the end, each lane looks its row up.  Rows behind the last repeat it
+    // (they count nothing), so every load is issued.
+    constexpr int RPI = 64 / ka.CH;
+    const bool wide_pages = (1 << pg.shift) >= RPI;
+    const uint32_t lane_at = lane * 16;
     auto issue = [&](int n0) {
+        if (wide_pages && n0 + KB <= t1) {
 #pragma unroll
-        for (int i = 0; i < ka.N; ++i) {
-            const size_t row = pages.row(min(n0 + ka.row_of(i, lane), t1 - 1));
-            ka.load(i, lane, pg.k, row);
-            va.load(i, lane, pg.v, row);
+            for (int i = 0; i < ka.N; ++i) {
+                const size_t at = pages.uniform_row(n0 + i * RPI) * (ka.CH * 16);
+                ka.x[i] = load16_stream(pg.k + at + lane_at);
+                va.x[i] = load16_stream(pg.v + at + lane_at);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < ka.N; ++i) {
+                const size_t at = pages.row(min(n0 + ka.row_of(i, lane), t1 - 1)) * (ka.CH * 16) + ka.piece_of(i, lane) * 16;
+                ka.x[i] = load16_stream(pg.k + at);
+                va.x[i] = load16_stream(pg.v + at);
+            }
         }
         if constexpr (CODES) ex = (lane < 32 ? pg.k_exp : pg.v_exp)[pages.row(min(n0 + (lane & 31), t1 - 1))];
     };
@@ -699,7 +718,7 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
             den += sc * wl[w * ROWS + r];
         }
         if (it.shares == 1) {
-            store_out<PARTS>(ck, (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + e, num / den);
+            store_out<PARTS>(ck, query_at(s, ck, bl, kvh, r, D) + e, num / den);
         } else {
             store_shared(mine + r * (D + 2) + 2 + e, num);
             if (e == 0) {
@@ -759,6 +778,11 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
     uint32_t ke[ka.N], ve[ka.N];  // codes: the rows' exponent bytes
     // Rows behind the last repeat it (they count nothing), so every load is issued.  With bf16 pages new rows come from
     // the inputs, at a stride of their own: addresses first, by the kind of tile (uniform branches), then the loads.
+    // A load instruction of a wave takes RPI rows: where they are one page's, their address is one scalar.
+    constexpr int RPI = 64 / ka.CH;
+    const bool wide_pages = (1 << pg.shift) >= RPI;
+    const int row0 = __builtin_amdgcn_readfirstlane(wave) * RPI;
+    const uint32_t lane_row = lane / ka.CH * (ka.CH * 16);
     const size_t new_row = (size_t)s.Hkv * D * 2;
     const size_t new0 = (((size_t)bl * ck.chunk - f) * s.Hkv + kvh) * D * 2;  // row n is at new0 + n new_row
     auto issue = [&](int n0) {
@@ -769,6 +793,17 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
                 const size_t at = new0 + (size_t)min(n0 + ka.row_of(i, tid), t1 - 1) * new_row;
                 kp[i] = reinterpret_cast<const uint8_t*>(ck.k_new) + at;
                 vp[i] = reinterpret_cast<const uint8_t*>(ck.v_new) + at;
+            }
+        } else if (wide_pages && n0 + KT <= min(t1, paged)) {
+#pragma unroll
+            for (int i = 0; i < ka.N; ++i) {
+                const size_t row = pages.uniform_row(n0 + i * RPI * 4 + row0);
+                kp[i] = pg.k + row * (D * code_bytes(KIND)) + lane_row;
+                vp[i] = pg.v + row * (D * code_bytes(KIND)) + lane_row;
+                if constexpr (KIND != kCacheBf16) {
+                    ke[i] = pg.k_exp[row + lane / ka.CH];
+                    ve[i] = pg.v_exp[row + lane / ka.CH];
+                }
             }
         } else {
 #pragma unroll
@@ -854,7 +889,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
         if (r >= rows) continue;
         if (it.shares == 1) {
             const float inv = 1.f / qr.l[nt];
-            const size_t at = (((size_t)bl * ck.chunk + r / s.G) * s.H + kvh * s.G + r % s.G) * D + 4 * qq;
+            const size_t at = query_at(s, ck, bl, kvh, r, D) + 4 * qq;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
                 const f32x4 v = qr.o[nt][db] * inv;

@@ -157,6 +157,10 @@ struct PageRows {
         for (int i = p0 + (int)threadIdx.x; i < p1; i += THREADS)
             lds[i - p0] = (uint32_t)pool_row(pg, s.Hkv, kvh, pg.table[(size_t)bl * pg.max_pages + i], 0);
     }
+    // row() of a row that is the same in every lane of the wave, as a scalar.
+    __device__ __forceinline__ size_t uniform_row(int n) const {
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)base[(n >> shift) - p0]) + (uint32_t)(n & ((1 << shift) - 1));
+    }
     __device__ __forceinline__ size_t row(int n) const { return base[(n >> shift) - p0] + (uint32_t)(n & ((1 << shift) - 1)); }
 };
 

@@ -121,6 +121,7 @@ struct Chunk {
     const int32_t* steps;
     const int32_t* n_new;
     int32_t reserve, chunk;
+    uint32_t inv_g;  // 2^32 / G, rounded up (unused with G = 1)
     const uint16_t* q;      // [B][L][chunk][H][D]
     const uint16_t* k_new;  // [B][L][chunk][H_kv][D]
     const uint16_t* v_new;
