@@ -744,6 +744,8 @@ __device__ __forceinline__ void put_bf16(char* p, const u32x4& x, float sc) {
     }
 }
 
+constexpr int kStreamChunk = 32;
+
 // A workgroup per (segment, KV head, 64 NT query rows), and per share of its keys.
 template <int D, int KIND, int NT, int PARTS>
 __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s, Pages pg, Chunk ck, Shares sh, int tiles) {
@@ -778,11 +780,6 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
     uint32_t ke[ka.N], ve[ka.N];  // codes: the rows' exponent bytes
     // Rows behind the last repeat it (they count nothing), so every load is issued.  With bf16 pages new rows come from
     // the inputs, at a stride of their own: addresses first, by the kind of tile (uniform branches), then the loads.
-    // A load instruction of a wave takes RPI rows: where they are one page's, their address is one scalar.
-    constexpr int RPI = 64 / ka.CH;
-    const bool wide_pages = (1 << pg.shift) >= RPI;
-    const int row0 = __builtin_amdgcn_readfirstlane(wave) * RPI;
-    const uint32_t lane_row = lane / ka.CH * (ka.CH * 16);
     const size_t new_row = (size_t)s.Hkv * D * 2;
     const size_t new0 = (((size_t)bl * ck.chunk - f) * s.Hkv + kvh) * D * 2;  // row n is at new0 + n new_row
     auto issue = [&](int n0) {
@@ -793,17 +790,6 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
                 const size_t at = new0 + (size_t)min(n0 + ka.row_of(i, tid), t1 - 1) * new_row;
                 kp[i] = reinterpret_cast<const uint8_t*>(ck.k_new) + at;
                 vp[i] = reinterpret_cast<const uint8_t*>(ck.v_new) + at;
-            }
-        } else if (wide_pages && n0 + KT <= min(t1, paged)) {
-#pragma unroll
-            for (int i = 0; i < ka.N; ++i) {
-                const size_t row = pages.uniform_row(n0 + i * RPI * 4 + row0);
-                kp[i] = pg.k + row * (D * code_bytes(KIND)) + lane_row;
-                vp[i] = pg.v + row * (D * code_bytes(KIND)) + lane_row;
-                if constexpr (KIND != kCacheBf16) {
-                    ke[i] = pg.k_exp[row + lane / ka.CH];
-                    ve[i] = pg.v_exp[row + lane / ka.CH];
-                }
             }
         } else {
 #pragma unroll
@@ -826,11 +812,24 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
                 }
             }
         }
+        // Where the call is a read of the retained rows, once (one row tile per unit, few tokens), they are streamed: 5 tokens
+        // on the video shape 67 us against 75.  Several tiles find the keys in L2, and with more tokens, whose
+        // rows are read again to be written to the pages, plain loads are faster: 64 tokens of the LLaVA-NeXT shape
+        // 185 us against 199.
+        if (NT == 1 && ck.chunk < kStreamChunk) {
+            asm volatile("; streamed");  // the compiler would merge the two branches' loads, and drop the hint
 #pragma unroll
-        for (int i = 0; i < ka.N; ++i) {
-            // one row tile per unit (NT = 1) reads its keys once; several find them in L2
-            ka.x[i] = load16_global<NT == 1>(kp[i] + ka.piece_of(i, tid) * 16);
-            va.x[i] = load16_global<NT == 1>(vp[i] + ka.piece_of(i, tid) * 16);
+            for (int i = 0; i < ka.N; ++i) {
+                ka.x[i] = load16_global<true>(kp[i] + ka.piece_of(i, tid) * 16);
+                va.x[i] = load16_global<true>(vp[i] + ka.piece_of(i, tid) * 16);
+            }
+            asm volatile("; streamed");
+        } else {
+#pragma unroll
+            for (int i = 0; i < ka.N; ++i) {
+                ka.x[i] = load16_global<false>(kp[i] + ka.piece_of(i, tid) * 16);
+                va.x[i] = load16_global<false>(vp[i] + ka.piece_of(i, tid) * 16);
+            }
         }
     };
     if (t0 < t1) issue(t0);
@@ -984,7 +983,7 @@ hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipS
     return hipGetLastError();
 }
 
-constexpr int kFineParts = 2;  // bf16 parts of a probability with 32-bit results
+constexpr int kFineParts = 3;  // bf16 parts of a probability with 32-bit results: all of its 24 bits
 
 template <int D, int KIND>
 hipError_t launch_chunk_k(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
