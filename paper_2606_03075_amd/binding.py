@@ -405,6 +405,12 @@ def _pages(pool, problem):
                       _ptr(pool.k_exp, _U8, "k_exp"), _ptr(pool.v_exp, _U8, "v_exp"), n, pool.page_size, pool.kind)
 
 
+def _on_current_device(t, name):
+    """The kernels run on the current device: a tensor elsewhere is refused, not reached over the fabric."""
+    if t.get_device() != _torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {t.get_device()}, not on the current one")
+
+
 def _sized(t, n, name):
     """t, after checking that it holds n elements."""
     if t is None or t.numel() != n:
@@ -420,10 +426,12 @@ def chunk_workspace_size(problem, opts, chunk) -> int:
 def tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream=None,
                         unit_order=None):
     """tgvkv_compact_paged into a PagedPool of any kind (8-bit kinds: quantised as written)."""
+    desc = _pages(pool, problem)
+    _on_current_device(pool.k_pool, "the pool")
     st = load_library().tgvkv_compact_pages(ctypes.byref(problem), _opts_ref(opts), _ptr(k, _BF16, "k"),
                                             _ptr(v, _BF16, "v"), _ptr(idx, _I32, "idx"),
                                             _ptr(budgets, _I32, "budgets"), _ptr(idx_offsets, _I64, "idx_offsets"),
-                                            int(total_budget), ctypes.byref(_pages(pool, problem)),
+                                            int(total_budget), ctypes.byref(desc),
                                             _ptr(block_table, _I32, "block_table"), _table_width(block_table, problem),
                                             _ptr(unit_order, _I32, "unit_order"), _stream(stream))
     _check("tgvkv_compact_pages", st)
@@ -431,13 +439,15 @@ def tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_bu
 
 def tgvkv_read_pages(problem, opts, pool, block_table, first, count, seg_offsets, k_out, v_out, stream=None):
     """Rows of a PagedPool's segments, first (None: 0) .. first + count, as contiguous bf16 segments."""
+    desc = _pages(pool, problem)
+    _on_current_device(pool.k_pool, "the pool")
     n = problem.batch * problem.layers
     if first is not None:
         _sized(first, n, "first")
     if k_out is None or v_out is None or k_out.numel() != v_out.numel():
         raise ValueError("k_out and v_out must hold the same number of elements")
     rows = k_out.numel() // (problem.heads_kv * problem.head_dim)
-    st = load_library().tgvkv_read_pages(ctypes.byref(problem), _opts_ref(opts), ctypes.byref(_pages(pool, problem)),
+    st = load_library().tgvkv_read_pages(ctypes.byref(problem), _opts_ref(opts), ctypes.byref(desc),
                                          _ptr(block_table, _I32, "block_table"), _table_width(block_table, problem),
                                          _ptr(first, _I32, "first"), _ptr(_sized(count, n, "count"), _I32, "count"),
                                          _ptr(_sized(seg_offsets, n + 1, "seg_offsets"), _I64, "seg_offsets"), rows,
@@ -451,6 +461,8 @@ def tgvkv_chunk_attn_pages(problem, opts, pool, block_table, budgets, decode_res
     heads_q, head_dim] for one token), k_new, v_new with heads_kv; n_new None: chunk tokens each.  out's type
     (float32 or bfloat16) is the result's."""
     p = problem
+    desc = _pages(pool, problem)
+    _on_current_device(pool.k_pool, "the pool")
     chunk = 1 if q.dim() == 4 else int(q.shape[2])
     tokens = p.batch * p.layers * chunk * p.head_dim
     _sized(q, tokens * p.heads_q, "q")
@@ -465,8 +477,7 @@ def tgvkv_chunk_attn_pages(problem, opts, pool, block_table, budgets, decode_res
         raise ValueError("unit_order must hold batch * layers elements")
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     st = load_library().tgvkv_chunk_attn_pages(ctypes.byref(problem), _opts_ref(opts),
-                                               ctypes.byref(_pages(pool, problem)),
-                                               _ptr(block_table, _I32, "block_table"),
+                                               ctypes.byref(desc), _ptr(block_table, _I32, "block_table"),
                                                _table_width(block_table, problem), _ptr(budgets, _I32, "budgets"),
                                                int(decode_reserve), _ptr(steps, _I32, "steps"),
                                                _ptr(n_new, _I32, "n_new"), chunk, _ptr(q, _BF16, "q"),

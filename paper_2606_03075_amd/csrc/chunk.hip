@@ -128,7 +128,7 @@ struct QueryRows {
     using B = Block<D, CODES>;
     bf16x8 qf[NT][D / 32];  // B operand of S^T: 8 dims of the lane's quarter per step
     f32x4 o[NT][D / 16];    // O^T: dims 16 db + 4 (l / 16) + {0..3}
-    float m[NT], l[NT];     // running maximum (base-2 logits) and the lane quarter's share of the sum
+    float m[NT], l[NT];     // reference of the exponents (base-2 logits, see raise) and the lane quarter's share of the sum
     int lim[NT];            // last visible row
 
     // First of the 8 dims of step ks in lane quarter qq.  A read of 16 codes feeds two steps.
@@ -202,9 +202,9 @@ struct QueryRows {
         }
     }
 
-    // MASK: rows n0 + .. above lim, or from `end` on, get -inf.  Then the rows' maxima.  A row's maximum moves only when a
-    // logit is kSlack above it: the probabilities are then at most 2^kSlack, which costs no precision in
-    // floating point, and most steps rescale nothing.
+    // MASK: rows n0 + .. above lim, or from `end` on, get -inf.  Then the rows' references: a row's reference is kSlack above
+    // the largest logit that moved it, so the probabilities stay at most 1, most steps move nothing, and what they lie
+    // below 1 costs no precision in floating point.
     template <bool MASK, int NB>
     __device__ __forceinline__ void raise(f32x4 (&a)[NB][NT], int n0, int end, float scale2) {
         const int qq = (threadIdx.x & 63) >> 4;
@@ -223,12 +223,12 @@ struct QueryRows {
                     mb[nt] = fmaxf(mb[nt], a[b][nt][j]);
                 }
             mb[nt] = max_xor32(max_xor16(mb[nt])) * scale2;
-            grew |= mb[nt] > m[nt] + kSlack;
+            grew |= mb[nt] > m[nt];
         }
         if (__builtin_amdgcn_ballot_w64(grew) != 0) {  // uniform branch
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float mn = fmaxf(m[nt], mb[nt]), sc = mn == kNegInf ? 1.f : fast_exp2(m[nt] - mn);
+                const float mn = mb[nt] > m[nt] ? mb[nt] + kSlack : m[nt], sc = mn == kNegInf ? 1.f : fast_exp2(m[nt] - mn);
                 l[nt] *= sc;
 #pragma unroll
                 for (int db = 0; db < D / 16; ++db) o[nt][db] *= sc;
@@ -433,11 +433,14 @@ __device__ __forceinline__ bool take_share(const Shape& s, const Pages& pg, cons
     // every thread has the segments of its own run
     const int n = s.B * s.L, per = (n + kThreads - 1) / kThreads, heads = s.Hkv * tiles;
     const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    unsigned long long total = 0;
-    for (int i = i0; i < i1; ++i) {
+    auto read_length = [&](int i) {
         const Part p = part_of(s, pg, ck, i);
-        total += (unsigned)(p.first + p.count);
-    }
+        return p.first + p.count;
+    };
+    const int length0 = i0 < i1 ? read_length(i0) : 0;  // the only one of up to 256 segments
+    auto length = [&](int i) { return i == i0 ? length0 : read_length(i); };
+    unsigned long long total = 0;
+    for (int i = i0; i < i1; ++i) total += (unsigned)length(i);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
     if (lane == 0) total_w[wave] = total;
@@ -448,8 +451,7 @@ __device__ __forceinline__ bool take_share(const Shape& s, const Pages& pg, cons
     const int rows0 = max(kShareRows, least);
     int mine = 0;  // extras of the thread's run
     for (int i = i0; i < i1; ++i) {
-        const Part p = part_of(s, pg, ck, i);
-        const int len = p.first + p.count;
+        const int len = length(i);
         if (len > rows0) mine += ((len - 1) / rows_per_share(len, rows0)) * heads;
     }
     int before = mine;
@@ -463,8 +465,7 @@ __device__ __forceinline__ bool take_share(const Shape& s, const Pages& pg, cons
     before -= mine;
     for (int w = 0; w < wave; ++w) before += extra_w[w];
     for (int i = i0; i < i1; ++i) {
-        const Part p = part_of(s, pg, ck, i);
-        const int len = p.first + p.count;
+        const int len = length(i);
         const int k = len > rows0 ? (len - 1) / rows_per_share(len, rows0) : 0;
         const int x = (int)blockIdx.x - before;
         if (extra ? x >= 0 && x < k * heads : i == it.bl) {
@@ -927,6 +928,12 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
     if (it.shares > 1) join_shares<D, ROWS, PARTS>(s, ck, sh, it, r_end - r_beg, r_beg, reinterpret_cast<float*>(smem));
 }
 
+// Workgroups for further shares, in calls of up to so many items.  Few extras make long shares, and each costs its
+// scan whether there is a share for it or not: five tokens on the video shape (896 items, layers of 100 to 3500 rows)
+// 82 us with 256, 62 with 384, 60 with 448, 67 with 512, 76 with 1024; single tokens there on 8-bit pages 67, 54, 54,
+// 54 and 62 us.  More items than that even out by themselves, longest first.
+constexpr int kExtras = 448, kItemsOfExtras = 2048;
+
 // How a call is dealt out.
 struct Plan {
     bool few;        // few_kernel
@@ -943,7 +950,7 @@ Plan plan_chunk(const Shape& s, int32_t chunk) {
     p.tiles = p.few ? 1 : (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
     p.part_rows = (p.few ? 16 : 64) * p.nt;
     const long long items = units * p.tiles;
-    p.extras = items > 0 && items <= 2048 && (long long)s.B * s.L <= kScanSegments ? (p.few ? 768 : 512) : 0;
+    p.extras = items > 0 && items <= kItemsOfExtras && (long long)s.B * s.L <= kScanSegments ? kExtras : 0;
     return p;
 }
 

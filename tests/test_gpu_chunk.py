@@ -60,6 +60,29 @@ def test_chunk_few_long_segments(lib, hq, hkv, d, chunk, kind):
     check(c, out_bf16=True)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("chunk", [3, 40])
+def test_widest_table(lib, kind, chunk):
+    """4096 one-row pages, the widest table (its page ids lie in LDS beside the staged keys)."""
+    log(f"chunk widest table kind={kind} chunk={chunk}")
+    c = case(14, 1, 1, 4, 2, 128, chunk, kind, 1, [4096 - chunk - 2], [2], None, chunk + 2, order=False)
+    assert c["table"].shape[1] == 4096
+    check(c)
+
+
+@pytest.mark.parametrize("chunk", [3, 70])
+@pytest.mark.parametrize("size", [1e37, 1e-30])
+def test_large_and_small_values(lib, chunk, size):
+    """V of the largest and of small magnitudes: no product or sum leaves the range on the way."""
+    from tests.pages_util import bits
+    log(f"chunk values of {size}")
+    c = case(15, 1, 2, 6, 2, 128, chunk, bd.CACHE_BF16, 16, [90, 7], [0], None, chunk)
+    v = c["pool"].x[1].astype(np.uint32) << 16
+    c["pool"].x[1] = np.where(c["pool"].x[1] == 0x7FC1, 0x7FC1, bits(v.view(np.float32) * np.float32(size))).astype(np.uint16)
+    c["v_new"] = bits((c["v_new"].astype(np.uint32) << 16).view(np.float32) * np.float32(size))
+    check(c)
+
+
 def test_chunk_many_layers_uneven(lib):
     """Layers of very different budgets, some empty, in a given order."""
     rng = np.random.default_rng(4)
