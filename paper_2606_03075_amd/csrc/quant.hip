@@ -80,14 +80,14 @@ __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages 
     }
 }
 
-template <int D, int KIND>
-__global__ __launch_bounds__(kThreads) void read_pages_kernel(Shape s, Pages pg, const int32_t* __restrict__ first,
+template <int D, int KIND, int THREADS>
+__global__ __launch_bounds__(THREADS) void read_pages_kernel(Shape s, Pages pg, const int32_t* __restrict__ first,
                                                               const int32_t* __restrict__ count,
                                                               const int64_t* __restrict__ seg_off, int64_t out_rows,
                                                               int nsplit, uint16_t* __restrict__ kc, uint16_t* __restrict__ vc) {
     extern __shared__ uint32_t lds_pages[];
     constexpr int CPR = D / 8;
-    constexpr int RPP = kThreads / CPR;
+    constexpr int RPP = THREADS / CPR;
     int bid = blockIdx.x;
     const int split = bid % nsplit;
     bid /= nsplit;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void read_pages_kernel(Shape s, Pages pg,
     if (r_beg >= r_end) return;  // uniform, before any barrier
     const int cc = threadIdx.x % CPR, rl = threadIdx.x / CPR;
     PageRows pages;
-    pages.init<kThreads>(s, pg, bl, kvh, f + r_beg, f + r_end, lds_pages);
+    pages.init<THREADS>(s, pg, bl, kvh, f + r_beg, f + r_end, lds_pages);
     __syncthreads();
     const size_t dst0 = ((size_t)s0 * s.Hkv + (size_t)kvh * cap) * D + cc * 8;
     auto move = [&](auto passes, int r0) {
@@ -175,18 +175,23 @@ hipError_t launch_read_pages(const Shape& s, const Pages& pg, const int32_t* fir
     if (out_rows <= 0 || s.B * s.L == 0) return hipSuccess;
     const int nsplit = row_splits(s, out_rows);
     const dim3 grid((unsigned)((long long)s.B * s.L * s.Hkv * nsplit));
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds_pages_bytes(pg), st, s, pg, first, count, seg_off, out_rows, nsplit, kc, vc);
+    auto launch = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), lds_pages_bytes(pg), st, s, pg, first, count, seg_off, out_rows,
+                           nsplit, kc, vc);
     };
-    if (s.D == 128) {
-        if (pg.kind == kCacheBf16) launch(read_pages_kernel<128, kCacheBf16>);
-        else if (pg.kind == kCacheFp8) launch(read_pages_kernel<128, kCacheFp8>);
-        else launch(read_pages_kernel<128, kCacheInt8>);
-    } else {
-        if (pg.kind == kCacheBf16) launch(read_pages_kernel<64, kCacheBf16>);
-        else if (pg.kind == kCacheFp8) launch(read_pages_kernel<64, kCacheFp8>);
-        else launch(read_pages_kernel<64, kCacheInt8>);
-    }
+    // segments of a few rows (what a step or a chunk appended) are work for one wave: 4096 of one row take 4.8 us, in four waves each 7.2
+    auto pick = [&](auto d, auto kind) {
+        constexpr int D = decltype(d)::value, KIND = decltype(kind)::value;
+        if (out_rows <= (int64_t)s.B * s.L * (8 * 64 / D)) launch(read_pages_kernel<D, KIND, 64>, 64);
+        else launch(read_pages_kernel<D, KIND, kThreads>, kThreads);
+    };
+    auto pick_kind = [&](auto d) {
+        if (pg.kind == kCacheBf16) pick(d, std::integral_constant<int, kCacheBf16>());
+        else if (pg.kind == kCacheFp8) pick(d, std::integral_constant<int, kCacheFp8>());
+        else pick(d, std::integral_constant<int, kCacheInt8>());
+    };
+    if (s.D == 128) pick_kind(std::integral_constant<int, 128>());
+    else pick_kind(std::integral_constant<int, 64>());
     return hipGetLastError();
 }
 
