@@ -929,7 +929,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
 }
 
 // Workgroups for further shares, in calls of up to so many items.  Few extras make long shares, and each costs its
-// scan whether there is a share for it or not: five tokens on the video shape (896 items, layers of 100 to 3500 rows)
+// scan whether there is a share for it or not: five tokens on the video shape (896 items, layers of 139 to 5449 rows)
 // 82 us with 256, 62 with 384, 60 with 448, 67 with 512, 76 with 1024; single tokens there on 8-bit pages 67, 54, 54,
 // 54 and 62 us.  More items than that even out by themselves, longest first.
 constexpr int kExtras = 448, kItemsOfExtras = 2048;

@@ -5,7 +5,7 @@
 // on the vector units, and each writes 8 codes; the row's first lane writes its exponent byte.
 // read_pages_kernel goes the other way, from pages of any kind to contiguous bf16 rows.  Each thread keeps
 // kPasses rows' K and V in flight (one row at a time was bound by latency: 298 us to store and 384 us to read
-// 1.2 M rows of 128, layers of 30 to 2979 rows), and page ids are looked up in LDS.
+// 1.2 M rows of 128, layers of 120 to 2979 rows), and page ids are looked up in LDS.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(THREADS) void read_pages_kernel(Shape s, Pages pg, 
 }
 
 // Workgroups per (sequence, layer, KV head): about one per 64 rows of the mean segment.  Segments differ in
-// length by an order of magnitude, and small shares even that out (1.2 M rows in 4096 units of 30 to 2979: 200 us
+// length by an order of magnitude, and small shares even that out (1.2 M rows in 4096 units of 120 to 2979: 200 us
 // with 4 each, 300 with one), but workgroups without rows are not free: 16384 of them take 40 us.
 int row_splits(const Shape& s, int64_t rows_total) {
     const long long units = (long long)s.B * s.L * s.Hkv, mean = rows_total / std::max<long long>((long long)s.B * s.L, 1);
