@@ -429,13 +429,13 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
  * A sequence takes no part, and its pages and rows of out are not touched, unless steps[b] >= 0,
  * 1 <= c <= chunk and steps[b] + c <= decode_reserve; nor does a segment whose table row is too narrow
  * for its f + c rows.  Tokens i >= c of the inputs are not read and their rows of out not touched.  A new
- * row whose table entry is outside [0, n_pages) is not written.  Of `problem`, only batch, layers, heads and
+ * row whose table entry is outside [0, n_pages) is not written (and results that see it are wrong).  Of `problem`, only batch, layers, heads and
  * head_dim are used, as in tgvkv_decode_attn_paged.
  *
  * q            bf16 [B][L][chunk][heads_q][head_dim];  k_new, v_new bf16 [B][L][chunk][heads_kv][head_dim]
  * steps, n_new_or_null  int32 [B], device
  * out          [B][L][chunk][heads_q][head_dim], f32, or bf16 with out_bf16 != 0 (the probabilities then enter
- *              the product with the values in bf16 too, which halves that product's work)
+ *              the product with the values in bf16 too, not in three bf16 parts)
  * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1 (TGVKV_E_UNSUPPORTED).
  * workspace >= tgvkv_chunk_workspace_size(p, o, chunk) (may be 0 bytes), with any first contents; calls that
  * may overlap need a workspace each.  unit_order_or_null as for tgvkv_decode_attn. */

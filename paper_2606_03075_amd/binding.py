@@ -463,6 +463,8 @@ def tgvkv_chunk_attn_pages(problem, opts, pool, block_table, budgets, decode_res
     p = problem
     desc = _pages(pool, problem)
     _on_current_device(pool.k_pool, "the pool")
+    if q.dim() not in (4, 5):
+        raise ValueError("q must be [batch, layers, chunk, heads_q, head_dim], or without chunk for one token")
     chunk = 1 if q.dim() == 4 else int(q.shape[2])
     tokens = p.batch * p.layers * chunk * p.head_dim
     _sized(q, tokens * p.heads_q, "q")

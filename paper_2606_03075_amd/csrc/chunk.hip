@@ -10,19 +10,21 @@
 //                 product's sum is free, so slot j of a lane quarter is the key that the quarter holds; V^T
 //                 comes from row-major V rows in LDS by transposing reads.  O's columns are rows of the
 //                 softmax, so a new maximum rescales a lane's values by the lane's own factor.
-// With 32-bit results the probabilities enter as two bf16 parts (16 significant bits), two products; with
-// bf16 results as one, whose 2^-9 is of the size of the result's own rounding.
+// With 32-bit results the probabilities enter as three bf16 parts, all of their 24 bits (errors of 2e-7 against 64 bits;
+// two parts left 2e-6, and three take 0 to 2 % longer where the cache is read, 8 % where products bound the
+// call); with bf16 results as one, off by 2^-8 at most like the result itself.
 //
-// K and V rows reach LDS as bf16 whatever the pages hold: an 8-bit code times its row's power of two is a
-// bf16, so the arithmetic behind the staging is the same for every kind.  LDS rows are padded so that both
-// kinds of read are free of bank conflicts: K rows by 16 bytes (16 rows at one column), V rows by 32 (the
-// transposing read takes 32 bytes of 8 rows at a time).
+// An 8-bit code times its row's power of two is a bf16, so the products take bf16 whatever the pages hold.
 //
-// Two kernels:
+// Two kernels (measured on MI355X):
 //   few_kernel   up to 32 query rows (drafted tokens, single tokens): a stream of the cache.  Every wave holds all
-//                rows and takes every fourth block of 32 keys, staged in LDS of its own, no barrier; the
-//                new rows are one more block, quantised and written to the pages on the way.
-//   rows_kernel  more: a wave holds 16 NT rows of its own and the workgroup's keys are staged for all.
+//                rows and takes every fourth block of 32 keys, staged in LDS of its own, no barrier; codes stay codes
+//                in LDS (half of it: three workgroups per CU instead of two).  The new rows are one more block,
+//                quantised and written to the pages on the way.  4096 units of 215 rows of e4m3, one query row each:
+//                56 us, 4.2 TB/s; the loads alone take 43.  Bound by instruction issue (76 % busy) and the units' set-up.
+//   rows_kernel  more: a wave holds 16 NT rows of its own, and 64 keys at a time are staged as bf16 for the workgroup.
+//                1000 tokens of 4 sequences, 28 layers, 28/4 heads of 128, bf16 results: 2.1 ms, 740 TFLOP/s.  Bound by
+//                what two waves per SIMD overlap of LDS waits, exponentials and products.
 //
 // A value that is not finite in a new token's V would reach earlier tokens through 0 * inf; such elements
 // are staged as 0 and added to the rows that see them at the end (rare: one flag is looked at).
@@ -116,12 +118,12 @@ __device__ __forceinline__ void drop_non_finite(u32x4& r) {
         r[i] = ((r[i] & 0x7F80u) == 0x7F80u ? 0u : r[i] & 0xFFFFu) | ((r[i] & 0x7F800000u) == 0x7F800000u ? 0u : r[i] & 0xFFFF0000u);
 }
 
-// 16 NT query rows of one (segment, KV head) in a wave, row 16 nt + l % 16 in lane l.  Keys come as bf16 rows in LDS
-// (CODED = kCacheBf16) or as codes of that kind with their rows' powers of two beside them.  PARTS: bf16 parts of
-// a probability in the product with V.
 // For sched_barrier: vector and scalar arithmetic may cross, matrix and LDS instructions stay in order.
 constexpr int kAluMayCross = 0x2 | 0x4;
 
+// 16 NT query rows of one (segment, KV head) in a wave, row 16 nt + l % 16 in lane l.  Keys come as bf16 rows in LDS
+// (CODED = kCacheBf16) or as codes of that kind with their rows' powers of two beside them.  PARTS: bf16 parts of
+// a probability in the product with V.
 template <int D, int NT, int PARTS, int CODED>
 struct QueryRows {
     static constexpr bool CODES = CODED != kCacheBf16;
@@ -409,7 +411,7 @@ __device__ __forceinline__ int rows_per_share(int len, int least) {
     return max(least, ((len + kMaxShares - 1) / kMaxShares + 63) / 64 * 64);
 }
 
-// The item and share of a workgroup; false: none.  `item` is the workgroup's own item where it is not an extra.  Called by
+// The item and share of a workgroup; false: none.  `unit`, `tile`: its own item where it is not an extra.  Called by
 // all threads, with the same arguments.
 __device__ __forceinline__ bool take_share(const Shape& s, const Pages& pg, const Chunk& ck, const Shares& sh, int tiles,
                                            int units, int unit, int tile, Item& it) {
@@ -956,6 +958,15 @@ Plan plan_chunk(const Shape& s, int32_t chunk) {
 
 size_t partial_floats(const Shape& s, const Plan& p) { return (size_t)2 * p.extras * p.part_rows * (s.D + 2); }
 
+// A number that no other call of the process has; never 0.
+unsigned long long call_number() {
+    static std::atomic<unsigned long long> next{
+        (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
+    unsigned long long call;
+    do call = next.fetch_add(1, std::memory_order_relaxed); while (call == 0);
+    return call;
+}
+
 template <int D, int KIND, int PARTS>
 hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
     const Plan p = plan_chunk(s, ck.chunk);
@@ -963,9 +974,7 @@ hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipS
     const size_t lds = lds_pages_bytes(pg);
     Shares sh{nullptr, nullptr, 0, p.extras};
     if (p.extras > 0) {
-        static std::atomic<unsigned long long> next{
-            (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
-        do sh.call = next.fetch_add(1, std::memory_order_relaxed); while (sh.call == 0);
+        sh.call = call_number();
         sh.part = ck.ws;
         sh.marks = reinterpret_cast<unsigned long long*>(ck.ws + partial_floats(s, p));
     }

@@ -202,7 +202,8 @@ def tolerance(c, out, mag, qk, out_bf16):
 
     A logit is d products summed in 32 bits: (d + 2) 2^-24 sum|q k| / sqrt(d), which changes a probability by
     that share, and its normaliser by as much again.  exp2 and the sums over n rows add (n + 8) 2^-23.  With
-    32-bit results the probabilities enter the product with V as two bf16 parts, 16 significant bits: 2^-16.  With bf16 results they
+    32-bit results the probabilities enter the product with V as bf16 parts, two in decode's own call (16 significant
+    bits: 2^-16), three here.  With bf16 results they
     are one bf16, off by 2^-8 at most, and the result is rounded once more, by 2^-8 of itself at most.
     """
     n = max(f + m for f, m in parts(c))
