@@ -285,6 +285,42 @@ def test_graph_replays(lib, hq, hkv, chunk, kind):
         assert torch.equal(x[2][8], want[rep % 2]), rep
 
 
+@pytest.mark.parametrize("hq,hkv,chunk,kind", [(7, 1, 3, bd.CACHE_FP8), (4, 2, 40, bd.CACHE_INT8), (16, 2, 40, bd.CACHE_BF16)])
+def test_a_serving_graph(lib, hq, hkv, chunk, kind):
+    """One captured call whose steps and n_new change between replays, as a loop around it does: sequences pause and
+    come back, so long segments are cut into shares in one replay and take no part in the next."""
+    import torch
+    log(f"chunk serving graph hq={hq} hkv={hkv} chunk={chunk} kind={kind}")
+    c = case(25, 2, 2, hq, hkv, 128, chunk, kind, 16, [3000, 411, 2200, 5], [3 * chunk, 3 * chunk], None, 4 * chunk)
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    b16 = lambda a: up(a.view(np.int16)).view(torch.bfloat16)  # noqa: E731
+    p = bd.make_problem(2, 2, hq, hkv, 128, 1, 0, 0)
+    size = bd.chunk_workspace_size(p, None, chunk)
+    pool, steps = c["pool"].device(), torch.zeros(2, dtype=torch.int32, device="cuda")
+    n_new, out = torch.full_like(steps, chunk), torch.empty(c["q"].shape, device="cuda")
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    args = (up(c["table"]), up(c["budgets"]), c["reserve"], steps, n_new, b16(c["q"]), b16(c["k_new"]), b16(c["v_new"]), out)
+    pool.extend(p, None, *args, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pool.extend(p, None, *args, ws)
+    for st, n in [((0, 0), (chunk, chunk)), ((chunk, chunk), (2, 0)), ((chunk + 2, chunk), (0, 3)),
+                  ((chunk + 2, -1), (1, 3)), ((chunk + 3, chunk + 3), (chunk, chunk)), ((3 * chunk, 0), (chunk, 0))]:
+        steps.copy_(torch.tensor(st, dtype=torch.int32))
+        n_new.copy_(torch.tensor(n, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.fill_(float("nan"))
+        pool.extend(p, None, *args, torch.full((size,), 255, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int32), out.view(torch.int32)), (st, n)
+        for b in range(2):
+            here = 0 if st[b] < 0 else n[b]
+            assert not got[b, :, :here].isnan().any() and got[b, :, here:].isnan().all(), (st, n)
+
+
 def test_other_streams(lib):
     """Two calls at once, each on a stream of its own with a workspace of its own, and the stream argument."""
     import torch
