@@ -311,3 +311,27 @@ def test_pool_arguments_are_checked(lib):
         go()
     torch.cuda.synchronize()
     assert torch.all(out == 7.0)
+
+
+def test_memory_elsewhere_is_refused(lib, monkeypatch):
+    """Every tensor has to be in the current GPU's memory: host tensors, and a pool of another device than the current."""
+    import torch
+    log("pool on another device")
+    dev = lambda dtype, *shape: torch.zeros(*shape, dtype=dtype, device="cuda")  # noqa: E731
+    p = bd.make_problem(1, 1, 4, 2, 64, 1, 0, 0)
+    i32, b16 = torch.int32, torch.bfloat16
+    for kind in KINDS:
+        pool = bd.PagedPool(2, 64, 8, 4, kind=kind)
+        calls = [(pool.extend, [dev(i32, 1, 2), dev(i32, 1), 4, dev(i32, 1), dev(i32, 1), dev(b16, 1, 1, 1, 4, 64),
+                                dev(b16, 1, 1, 1, 2, 64), dev(b16, 1, 1, 1, 2, 64), dev(b16, 1, 1, 1, 4, 64),
+                                dev(torch.uint8, max(16, bd.chunk_workspace_size(p, None, 1)))]),
+                 (pool.read, [dev(i32, 1, 2), dev(i32, 1), dev(torch.int64, 2), dev(b16, 128), dev(b16, 128)])]
+        for f, args in calls:
+            for i, a in enumerate(args):
+                if torch.is_tensor(a):
+                    with pytest.raises(ValueError, match="memory"):
+                        f(p, None, *args[:i], a.cpu(), *args[i + 1:])
+            with monkeypatch.context() as m:
+                m.setattr(torch.cuda, "current_device", lambda: 1)
+                with pytest.raises(ValueError, match="current GPU"):
+                    f(p, None, *args)
