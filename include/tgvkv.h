@@ -15,8 +15,8 @@
  * The same cache can instead live in fixed-size pages of a shared pool, for
  * serving with continuous batching: tgvkv_page_plan, tgvkv_page_table,
  * tgvkv_compact_paged, tgvkv_decode_attn_paged; several new tokens per sequence
- * in one call, and pages that hold 8 bits: tgvkv_compact_pages, tgvkv_read_pages,
- * tgvkv_chunk_attn_pages.
+ * in one call, and pages that hold 8 bits: tgvkv_compact_pages, tgvkv_store_pages,
+ * tgvkv_read_pages, tgvkv_chunk_attn_pages.
  *
  * Conventions shared by every call
  *  - Token layout of each sequence: n_sys system-text tokens, then n_vis vision
@@ -402,6 +402,15 @@ tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts*
                                  const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
                                  int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
                                  int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream);
+
+/* tgvkv_store_pages -- tgvkv_compact_pages with a table of any width, such as one made for the budgets that the
+ * segments have: these are on the device, so the host can only tell the largest that total_budget allows, which is
+ * often several times the largest there is.  Rows behind the max_pages * page_size that a table row names are not
+ * stored; everything else is as there, the same bits included. */
+tgvkv_status tgvkv_store_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const void* k, const void* v,
+                               const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
+                               int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream);
 
 /* tgvkv_read_pages -- rows of paged segments as contiguous bf16, the values that they stand for.
  * For every (b, l), KV head h and n < count[b*L+l], row first[b*L+l] + n of the segment's pages goes to

@@ -29,7 +29,8 @@ ABI_VERSION = 9  # TGVKV_ABI_VERSION of the library this binding marshals for
 EXPORTS = ("tgvkv_score", "tgvkv_budget", "tgvkv_select", "tgvkv_compact", "tgvkv_decode_attn",
            "tgvkv_decode_attn_noalloc",
            "tgvkv_page_plan", "tgvkv_page_table", "tgvkv_compact_paged", "tgvkv_decode_attn_paged",
-           "tgvkv_compact_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages", "tgvkv_chunk_workspace_size",
+           "tgvkv_compact_pages", "tgvkv_store_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages",
+           "tgvkv_chunk_workspace_size",
            "tgvkv_sizes", "tgvkv_workspace_size", "tgvkv_status_string", "tgvkv_abi_version")
 # measurement kernels (include/tgvkv_ceiling.h): the chip's achievable stream and matrix-core rates
 CEILING_EXPORTS = ("tgvkv_ceiling_read", "tgvkv_ceiling_copy", "tgvkv_ceiling_mfma", "tgvkv_ceiling_mfma_flops")
@@ -91,6 +92,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                             vp, vp]
     D = ctypes.POINTER(TgvkvPages)
     lib.tgvkv_compact_pages.argtypes = [P, O, vp, vp, vp, vp, vp, i64, D, vp, i32, vp, vp]
+    lib.tgvkv_store_pages.argtypes = lib.tgvkv_compact_pages.argtypes
     lib.tgvkv_read_pages.argtypes = [P, O, D, vp, i32, vp, vp, vp, i64, vp, vp, vp]
     lib.tgvkv_chunk_attn_pages.argtypes = [P, O, D, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, i32, vp, sz, vp, vp]
     lib.tgvkv_chunk_workspace_size.argtypes = [P, O, i32]
@@ -108,7 +110,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.tgvkv_ceiling_mfma_flops.restype = ctypes.c_longlong
     for name in ("tgvkv_score", "tgvkv_budget", "tgvkv_select", "tgvkv_compact", "tgvkv_decode_attn",
                  "tgvkv_decode_attn_noalloc", "tgvkv_page_plan", "tgvkv_page_table", "tgvkv_compact_paged", "tgvkv_decode_attn_paged",
-                 "tgvkv_compact_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages",
+                 "tgvkv_compact_pages", "tgvkv_store_pages", "tgvkv_read_pages", "tgvkv_chunk_attn_pages",
                  "tgvkv_sizes", "tgvkv_abi_version", "tgvkv_ceiling_read", "tgvkv_ceiling_copy",
                  "tgvkv_ceiling_mfma"):
         getattr(lib, name).restype = ctypes.c_int32
@@ -443,17 +445,29 @@ def chunk_workspace_size(problem, opts, chunk) -> int:
     return int(load_library().tgvkv_chunk_workspace_size(ctypes.byref(problem), _opts_ref(opts), int(chunk)))
 
 
-def tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream=None,
-                        unit_order=None):
-    """tgvkv_compact_paged into a PagedPool of any kind (8-bit kinds: quantised as written)."""
+def _store(fn, problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream, unit_order):
     desc, device = _pages(pool, problem.heads_kv, problem.head_dim)
-    st = load_library().tgvkv_compact_pages(
+    st = getattr(load_library(), fn)(
         ctypes.byref(problem), _opts_ref(opts), _at(k, _BF16, None, device, "k"), _at(v, _BF16, None, device, "v"),
         _at(idx, _I32, None, device, "idx"), _at(budgets, _I32, None, device, "budgets"),
         _at(idx_offsets, _I64, None, device, "idx_offsets"), int(total_budget), ctypes.byref(desc),
         _at(block_table, _I32, None, device, "block_table"), _table_width(block_table, problem),
         _at(unit_order, _I32, None, device, "unit_order"), _stream_on(stream, device))
-    _check("tgvkv_compact_pages", st)
+    _check(fn, st)
+
+
+def tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream=None,
+                        unit_order=None):
+    """tgvkv_compact_paged into a PagedPool of any kind (8-bit kinds: quantised as written)."""
+    _store("tgvkv_compact_pages", problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream,
+           unit_order)
+
+
+def tgvkv_store_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream=None,
+                      unit_order=None):
+    """tgvkv_compact_pages with a table of any width; rows behind those that it names are not stored."""
+    _store("tgvkv_store_pages", problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream,
+           unit_order)
 
 
 def tgvkv_read_pages(problem, opts, pool, block_table, first, count, seg_offsets, k_out, v_out, stream=None):
@@ -667,13 +681,9 @@ class PagedPool:
         return table
 
     def store(self, problem, opts, k, v, idx, budgets, idx_offsets, total_budget, table, stream=None, unit_order=None):
-        """The retained rows of an evicted batch into the pages of its table, quantised with an 8-bit kind."""
-        if self.kind == CACHE_BF16:
-            tgvkv_compact_paged(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, table, self.page_size,
-                                self.k_pool, self.v_pool, stream, unit_order)
-        else:
-            tgvkv_compact_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, self, table, stream,
-                                unit_order)
+        """The retained rows of an evicted batch into the pages of its table, quantised with an 8-bit kind.  The table
+        may be as narrow as the longest segment needs; rows behind those that it names are not stored."""
+        tgvkv_store_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, self, table, stream, unit_order)
 
     def release(self, table_rows):
         """Return the pages of finished sequences' table rows to the free list."""

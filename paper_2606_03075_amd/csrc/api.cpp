@@ -199,6 +199,36 @@ bool pages_present(const tgvkv::Pages& pg) {
 
 tgvkv_status hip_status(hipError_t e) { return e == hipSuccess ? TGVKV_OK : TGVKV_E_HIP; }
 
+// tgvkv_compact_pages, and with any_width tgvkv_store_pages.
+tgvkv_status store_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const void* k, const void* v,
+                         const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets, int64_t total_budget,
+                         const tgvkv_pages* pages, const int32_t* block_table, int32_t max_pages,
+                         const int32_t* unit_order, bool any_width, hipStream_t stream) {
+    Shape s;
+    tgvkv_status st = make_shape(problem, opts, &s);
+    if (st != TGVKV_OK) return st;
+    tgvkv::Pages pg;
+    st = make_pages(pages, max_pages, block_table, &pg);
+    if (st != TGVKV_OK) return st;
+    if (total_budget < 0) return TGVKV_E_INVAL;
+    if (total_budget > budget_capacity(s)) return TGVKV_E_CAPACITY;
+    const bool wide = (max_layer_budget(s, total_budget) + pages->page_size - 1) / pages->page_size <= max_pages;
+    if (pg.kind == TGVKV_CACHE_BF16 && (wide || !any_width))
+        return tgvkv_compact_paged(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, block_table, max_pages,
+                                   pages->page_size, pages->k, pages->v, pages->n_pages, unit_order, stream);
+    if (!wide && !any_width) return TGVKV_E_CAPACITY;
+    const int64_t kept = kept_per_sequence(s, total_budget);
+    if (s.B == 0 || kept == 0) return TGVKV_OK;
+    if (k == nullptr || v == nullptr || idx == nullptr || budgets == nullptr || idx_offsets == nullptr ||
+        !pages_present(pg))
+        return TGVKV_E_INVAL;
+    if (!aligned16(k) || !aligned16(v)) return TGVKV_E_INVAL;
+    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    return hip_status(tgvkv::launch_compact_pages(s, pg, static_cast<const uint16_t*>(k),
+                                                  static_cast<const uint16_t*>(v), idx, budgets, idx_offsets,
+                                                  (int64_t)s.B * kept, unit_order, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -505,29 +535,16 @@ tgvkv_status tgvkv_compact_pages(const tgvkv_problem* problem, const tgvkv_opts*
                                  const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
                                  int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
                                  int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream) {
-    Shape s;
-    tgvkv_status st = make_shape(problem, opts, &s);
-    if (st != TGVKV_OK) return st;
-    tgvkv::Pages pg;
-    st = make_pages(pages, max_pages, block_table, &pg);
-    if (st != TGVKV_OK) return st;
-    if (pg.kind == TGVKV_CACHE_BF16)
-        return tgvkv_compact_paged(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, block_table, max_pages,
-                                   pages->page_size, pages->k, pages->v, pages->n_pages, unit_order_or_null, stream);
-    if (total_budget < 0) return TGVKV_E_INVAL;
-    if (total_budget > budget_capacity(s)) return TGVKV_E_CAPACITY;
-    if ((max_layer_budget(s, total_budget) + pages->page_size - 1) / pages->page_size > max_pages)
-        return TGVKV_E_CAPACITY;
-    const int64_t kept = kept_per_sequence(s, total_budget);
-    if (s.B == 0 || kept == 0) return TGVKV_OK;
-    if (k == nullptr || v == nullptr || idx == nullptr || budgets == nullptr || idx_offsets == nullptr ||
-        !pages_present(pg))
-        return TGVKV_E_INVAL;
-    if (!aligned16(k) || !aligned16(v)) return TGVKV_E_INVAL;
-    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
-    return hip_status(tgvkv::launch_compact_pages(s, pg, static_cast<const uint16_t*>(k),
-                                                  static_cast<const uint16_t*>(v), idx, budgets, idx_offsets,
-                                                  (int64_t)s.B * kept, unit_order_or_null, stream));
+    return store_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pages, block_table, max_pages,
+                       unit_order_or_null, false, stream);
+}
+
+tgvkv_status tgvkv_store_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const void* k, const void* v,
+                               const int32_t* idx, const int32_t* budgets, const int64_t* idx_offsets,
+                               int64_t total_budget, const tgvkv_pages* pages, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* unit_order_or_null, hipStream_t stream) {
+    return store_pages(problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pages, block_table, max_pages,
+                       unit_order_or_null, true, stream);
 }
 
 tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,

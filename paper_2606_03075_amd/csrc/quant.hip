@@ -1,7 +1,7 @@
 // The paged cache in 8 bits: the retained rows quantised as they are written, and rows read back.
 //
-// Both are HBM streams.  compact_pages_kernel is compact_kernel with a different store: a row of head_dim
-// bf16 is read by head_dim/8 lanes with 16-byte loads, the lanes agree on its largest magnitude by lane swaps
+// Both are HBM streams.  compact_pages_kernel is compact_kernel with a different store, and for tables of any width
+// (rows behind the table's are not stored): a row of head_dim bf16 is read by head_dim/8 lanes with 16-byte loads, the lanes agree on its largest magnitude by lane swaps
 // on the vector units, and each writes 8 codes; the row's first lane writes its exponent byte.
 // read_pages_kernel goes the other way, from pages of any kind to contiguous bf16 rows.  Each thread keeps
 // kPasses rows' K and V in flight (one row at a time was bound by latency: 298 us to store and 384 us to read
@@ -65,15 +65,23 @@ __global__ __launch_bounds__(kThreads) void compact_pages_kernel(Shape s, Pages 
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) {
             const int r = r0 + i * RPP + rl;
-            // every lane takes part in the row's maximum
-            const uint32_t ke = exp_byte<KIND>(group_max<CPR>(amax8(kr[i]))), ve = exp_byte<KIND>(group_max<CPR>(amax8(vr[i])));
-            if (r < r_end) {
-                const size_t row = pages.row(r);
-                *reinterpret_cast<u32x2*>(pg.k + row * D + cc * 8) = encode8<KIND>(kr[i], ke);
-                *reinterpret_cast<u32x2*>(pg.v + row * D + cc * 8) = encode8<KIND>(vr[i], ve);
-                if (cc == 0) {
-                    pg.k_exp[row] = (uint8_t)ke;
-                    pg.v_exp[row] = (uint8_t)ve;
+            if constexpr (KIND == kCacheBf16) {
+                if (r < r_end) {
+                    const size_t at = (pages.row(r) * D + cc * 8) * 2;
+                    store16(pg.k + at, kr[i]);
+                    store16(pg.v + at, vr[i]);
+                }
+            } else {
+                // every lane takes part in the row's maximum
+                const uint32_t ke = exp_byte<KIND>(group_max<CPR>(amax8(kr[i]))), ve = exp_byte<KIND>(group_max<CPR>(amax8(vr[i])));
+                if (r < r_end) {
+                    const size_t row = pages.row(r);
+                    *reinterpret_cast<u32x2*>(pg.k + row * D + cc * 8) = encode8<KIND>(kr[i], ke);
+                    *reinterpret_cast<u32x2*>(pg.v + row * D + cc * 8) = encode8<KIND>(vr[i], ve);
+                    if (cc == 0) {
+                        pg.k_exp[row] = (uint8_t)ke;
+                        pg.v_exp[row] = (uint8_t)ve;
+                    }
                 }
             }
         }
@@ -163,9 +171,12 @@ hipError_t launch_compact_pages(const Shape& s, const Pages& pg, const uint16_t*
     if (pg.kind == kCacheFp8) {
         if (s.D == 128) launch(compact_pages_kernel<128, kCacheFp8>);
         else launch(compact_pages_kernel<64, kCacheFp8>);
-    } else {
+    } else if (pg.kind == kCacheInt8) {
         if (s.D == 128) launch(compact_pages_kernel<128, kCacheInt8>);
         else launch(compact_pages_kernel<64, kCacheInt8>);
+    } else {  // tables too narrow for compact_kernel, which takes every row to have a page
+        if (s.D == 128) launch(compact_pages_kernel<128, kCacheBf16>);
+        else launch(compact_pages_kernel<64, kCacheBf16>);
     }
     return hipGetLastError();
 }

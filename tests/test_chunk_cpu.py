@@ -93,6 +93,35 @@ def test_store_and_read_refusals(so):
     assert store(problem=P(batch=0), pool=pages(k=None)) == read(problem=P(batch=0), pool=pages(k=None)) == 0
 
 
+@pytest.mark.skipif(_gpu(), reason="fake pointers are used only where no GPU exists")
+def test_a_store_takes_a_table_of_any_width(so):
+    """Refusals as tgvkv_compact_pages', but for the width.  (A null tensor behind the width check tells that it passed
+    without reaching a launch.)"""
+    def store(problem=None, pool=pages(), k=FAKE, v=FAKE, idx=FAKE, budgets=FAKE, offs=FAKE, total=10, table=FAKE, width=2,
+              call=None):
+        return (call or so.tgvkv_store_pages)(ctypes.byref(problem or P()), None, k, v, idx, budgets, offs, total, pool, table,
+                                              width, None, S)
+    for bad, code in BAD_POOLS:
+        assert store(pool=pages(**bad)) == code, bad
+    assert store(pool=None) == -1
+    for kind in (0, 1, 2):
+        pool = pages(kind=kind)
+        for bad, code in [(dict(k=None), -1), (dict(v=ODD), -1), (dict(idx=None), -1), (dict(budgets=None), -1),
+                          (dict(offs=None), -1), (dict(total=-1), -1), (dict(total=2 * 48 + 1), -4), (dict(width=0), -1),
+                          (dict(width=4097), -2), (dict(table=None), -1), (dict(problem=P(heads_q=3)), -1)]:
+            assert store(pool=pool, **bad) == code, (kind, bad)
+            assert store(pool=pool, width=bad.pop("width", 1), **bad) == code, (kind, bad)
+        assert store(pool=pool, width=1, idx=None, call=so.tgvkv_compact_pages) == -4
+    # one image question kept at a tenth: 32 layers share 2083 tokens, the longest holds 208 of them
+    image = P(layers=32, heads_q=32, heads_kv=32, n_sys=0, n_vis=651, n_qst=0)
+    need = bd.page_plan(image, None, 2083, 0, 16)[0]
+    assert need == 41
+    for width, code in ((13, -4), (41, -1)):
+        assert store(problem=image, pool=pages(size=16), total=2083, width=width, idx=None, call=so.tgvkv_compact_pages) == code
+        assert store(problem=image, pool=pages(size=16), total=2083, width=width, idx=None) == -1
+    assert store(problem=P(batch=0), pool=pages(k=None)) == 0
+
+
 def test_chunk_workspace_size(so):
     assert bd.chunk_workspace_size(P(head_dim=96), None, 1) == 0
     assert bd.chunk_workspace_size(P(), None, 0) == 0

@@ -142,6 +142,39 @@ def test_admit_and_read(lib, kind, page, heads, kw, rho, head_mode, vision_only)
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,page,head_mode", [(128, 16, 0), (64, 4, 1)])
+@pytest.mark.parametrize("drop", [0, 1, 100])
+def test_store_into_a_narrow_table(lib, kind, d, page, head_mode, drop):
+    """A table as wide as its longest segment needs, and narrower ones: the rows that it names are stored as into a wide
+    one, the others nowhere."""
+    import torch
+    log(f"narrow table kind={kind} d={d} page={page} head_mode={head_mode} drop={drop}")
+    rng = np.random.default_rng(7)
+    B, L, hkv, N = 2, 3, 2, 300
+    bud = np.array([[40, 130, 10], [1, 90, 89]], np.int32)  # one layer may hold all 180 of a sequence
+    k, v = (bits(rng.standard_normal((B, L, hkv, N, d))) for _ in range(2))
+    longest = -(-int(bud.max()) // page)
+    width = max(1, longest - drop)
+    p, o = bd.make_problem(B, L, hkv, hkv, d, 0, N, 0), bd.make_opts(head_mode=head_mode)
+    assert width < bd.page_plan(p, o, 180, 0, page)[0]
+    ref = Pool(B * L * longest + 2, hkv, page, d, kind)
+    table = rng.permutation(B * L * longest)[:B * L * width].reshape(B * L, width).astype(np.int32)
+    g = hkv if head_mode else 1
+    pick = [[np.sort(rng.choice(N, n, replace=False)) for _ in range(g)] for n in bud.reshape(-1)]
+    off = np.concatenate([[0], np.cumsum(bud.reshape(-1).astype(np.int64) * g)])
+    pool = ref.device()
+    pool.store(p, o, dev_bf16(k), dev_bf16(v), _up(np.concatenate([x for q in pick for x in q]).astype(np.int32)), _up(bud),
+               _up(off), 180, _up(table))
+    torch.cuda.synchronize()
+    for bl in range(B * L):
+        for w, x in enumerate((k, v)):
+            rows = np.stack([x.reshape(B * L, hkv, N, d)[bl, h][pick[bl][h if head_mode else 0]] for h in range(hkv)], 1)
+            for r in range(min(len(rows), width * page)):
+                ref.write(w, table[bl], r, rows[r])
+    ref.check(pool)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_read_parts(lib, kind):
     """Rows from `first` on, counts of nothing, above the segment's room and negative, pages that end inside."""
     import torch
