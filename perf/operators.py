@@ -164,13 +164,11 @@ def _order(b):
 
 
 def _table(c, b, r):
-    """The batch's pages, scattered over the pool: a table [B*L][max_pages], as wide as one layer's largest
-    possible budget needs (page_plan's width), and the pool's size."""
+    """The batch's pages, scattered over the pool: a table [B*L][max_pages] and the pool's size."""
     need = -(-(b.reshape(-1).astype(np.int64) + c["reserve"]) // c["page"])
     n_pages = (c["batch"] * (_total(c) + c["layers"] * (c["reserve"] + c["page"] - 1))) // c["page"]  # holds any split
     ids, at = r.permutation(n_pages).astype(np.int32), 0
-    width = -(-(min(c["tokens"], _total(c)) + c["reserve"]) // c["page"])
-    table = np.full((b.size, max(1, width)), -1, np.int32)
+    table = np.full((b.size, max(1, int(need.max()))), -1, np.int32)
     for i, n in enumerate(need):
         table[i, :n] = ids[at:at + n]
         at += n
