@@ -446,7 +446,8 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
  * out          [B][L][chunk][heads_q][head_dim], f32, or bf16 with out_bf16 != 0 (the probabilities then enter
  *              the product with the values in bf16 too, not in three bf16 parts)
  * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1 (TGVKV_E_UNSUPPORTED).
- * workspace >= tgvkv_chunk_workspace_size(p, o, chunk) (may be 0 bytes), with any first contents; calls that
+ * workspace >= tgvkv_chunk_workspace_size(p, o, chunk) (may be 0 bytes; TGVKV_E_WORKSPACE if it is less than this
+ * chunk needs), with any first contents; calls that
  * may overlap need a workspace each.  unit_order_or_null as for tgvkv_decode_attn. */
 tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,
                                     const int32_t* block_table, int32_t max_pages, const int32_t* budgets,
@@ -455,7 +456,9 @@ tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_op
                                     int32_t out_bf16, void* workspace, size_t workspace_bytes,
                                     const int32_t* unit_order_or_null, hipStream_t stream);
 
-/* Workspace bytes of tgvkv_chunk_attn_pages for chunks of up to `chunk` tokens; 0 for an invalid problem or chunk. */
+/* Workspace bytes of tgvkv_chunk_attn_pages for any chunk of up to `chunk` tokens: one workspace of the largest chunk's
+ * size serves a loop's drafts, questions and single tokens (not in calls that overlap).  0 for an invalid problem or
+ * chunk, and where no such call needs any. */
 size_t tgvkv_chunk_workspace_size(const tgvkv_problem* problem, const tgvkv_opts* opts, int32_t chunk);
 
 /* tgvkv_sizes -- host-only sizes that follow from the problem and options (no HIP call).

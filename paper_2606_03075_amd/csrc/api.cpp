@@ -570,7 +570,7 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
 size_t tgvkv_chunk_workspace_size(const tgvkv_problem* problem, const tgvkv_opts* opts, int32_t chunk) {
     Shape s;
     if (make_shape(problem, opts, &s) != TGVKV_OK || !chunk_fits(s, chunk)) return 0;
-    return align_up(tgvkv::chunk_workspace(s, chunk));
+    return align_up(tgvkv::chunk_workspace_up_to(s, chunk));
 }
 
 tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, const tgvkv_pages* pages,

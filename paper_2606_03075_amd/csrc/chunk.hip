@@ -1013,6 +1013,15 @@ size_t chunk_workspace(const Shape& s, int32_t chunk) {
     return sizeof(float) * partial_floats(s, p) + sizeof(unsigned long long) * 2 * (size_t)p.extras;
 }
 
+// The largest of the chunks up to `chunk`.  A partial's rows step up behind 16, 32 and 64 query rows, and among chunks of
+// the same the first has the fewest items: where it has no extras, none has.
+size_t chunk_workspace_up_to(const Shape& s, int32_t chunk) {
+    size_t most = 0;
+    for (const int32_t rows : {0, 16, 32, 64})
+        if (rows / s.G + 1 <= chunk) most = std::max(most, chunk_workspace(s, rows / s.G + 1));
+    return most;
+}
+
 hipError_t launch_chunk(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
     if ((long long)s.B * s.L == 0) return hipSuccess;
     if (s.D == 128) {

@@ -131,7 +131,8 @@ struct Chunk {
     float* ws;
 };
 
-size_t chunk_workspace(const Shape& s, int32_t chunk);
+size_t chunk_workspace(const Shape& s, int32_t chunk);        // bytes that a call with this chunk needs
+size_t chunk_workspace_up_to(const Shape& s, int32_t chunk);  // that any call with at most this chunk does
 hipError_t launch_chunk(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st);
 
 }  // namespace tgvkv

@@ -131,6 +131,26 @@ def test_chunk_workspace_size(so):
             assert 0 <= bd.chunk_workspace_size(P(batch=batch, layers=32), None, chunk) <= 1 << 30
 
 
+@pytest.mark.parametrize("g", [1, 4, 7, 16])
+@pytest.mark.parametrize("batch,layers,hkv", [(1, 1, 1), (1, 5, 2), (8, 28, 4), (4, 32, 8), (16, 40, 40), (64, 40, 1)])
+def test_one_workspace_serves_every_smaller_chunk(so, g, batch, layers, hkv):
+    """chunk_workspace_size is for chunks of UP TO its argument: it never falls as the argument grows, also where larger
+    chunks need none themselves.  Up to 2048 items (units times row tiles) a call needs 896 partials of the tile's rows
+    (16, 32, 64 or 128, by the chunk's query rows), each of head_dim + 2 floats, and a mark of 8 bytes each."""
+    p = P(batch=batch, layers=layers, heads_q=g * hkv, heads_kv=hkv)
+
+    def need(chunk):
+        rows = chunk * g
+        tile, tiles = (16, 1) if rows <= 16 else (32, 1) if rows <= 32 else (64, 1) if rows <= 64 else (128, -(-rows // 128))
+        if batch * layers * hkv * tiles > 2048 or batch * layers > 2048:
+            return 0
+        return -(-896 * (tile * (128 + 2) * 4 + 8) // 256) * 256
+    most = 0
+    for chunk in [*range(1, 300), 1000, 4096]:
+        most = max(most, need(chunk))
+        assert bd.chunk_workspace_size(p, None, chunk) == most, chunk
+
+
 def test_an_older_library_is_refused(tmp_path):
     """A library without the calls on pages of any kind does not load."""
     import subprocess

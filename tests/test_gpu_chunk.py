@@ -321,6 +321,25 @@ def test_a_serving_graph(lib, hq, hkv, chunk, kind):
             assert not got[b, :, :here].isnan().any() and got[b, :, here:].isnan().all(), (st, n)
 
 
+@pytest.mark.parametrize("kind", [bd.CACHE_BF16, bd.CACHE_INT8])
+def test_a_loop_keeps_one_workspace(lib, kind):
+    """A workspace made for the largest chunk, whose own calls need none (2560 items), and exactly as large as it is said
+    to be: single tokens, drafts and questions of every tile size on it."""
+    import torch
+    log(f"chunk one workspace kind={kind}")
+    B, L, hq, hkv, d = 8, 16, 8, 4, 64
+    p = bd.make_problem(B, L, hq, hkv, d, 1, 0, 0)
+    size = bd.chunk_workspace_size(p, None, 320)
+    assert size >= 896 * 128 * (d + 2) * 4
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    budgets = np.random.default_rng(3).integers(0, 3, (B, L)).astype(np.int32)
+    budgets[1, 3], budgets[6, 15] = 700, 300
+    for chunk, n_new in ((1, None), (320, [1, 3, 0, 0, 0, 0, 17, 0]), (8, [1, 8, 0, 0, 0, 2, 5, 0]), (12, [0, 12, 0, 0, 0, 0, 9, 1]),
+                         (32, [0, 32, 0, 0, 0, 0, 4, 0]), (40, [0, 7, 1, 0, 0, 0, 33, 0]), (1, None)):
+        log(f"  chunk={chunk}")
+        check(case(50 + chunk, B, L, hq, hkv, d, chunk, kind, 16, budgets, np.arange(B) % 3, n_new, chunk + 4), ws=ws)
+
+
 def test_other_streams(lib):
     """Two calls at once, each on a stream of its own with a workspace of its own, and the stream argument."""
     import torch
