@@ -27,7 +27,8 @@
 //                what two waves per SIMD overlap of LDS waits, exponentials and products.
 //
 // A value that is not finite in a new token's V would reach earlier tokens through 0 * inf; such elements
-// are staged as 0 and added to the rows that see them at the end (rare: one flag is looked at).
+// are staged as 0 and added to the rows that see them at the end (rare: one flag is looked at), after the last
+// rescaling: a factor or a probability too small for 32 bits times an infinity is a NaN, where the sum is infinite.
 #include <algorithm>
 #include <atomic>
 #include <chrono>
@@ -117,6 +118,9 @@ __device__ __forceinline__ void drop_non_finite(u32x4& r) {
     for (int i = 0; i < 4; ++i)
         r[i] = ((r[i] & 0x7F80u) == 0x7F80u ? 0u : r[i] & 0xFFFFu) | ((r[i] & 0x7F800000u) == 0x7F800000u ? 0u : r[i] & 0xFFFF0000u);
 }
+
+// A weighted sum taken to another reference: an infinity stays one, also where the factor has no 32 bits left.
+__device__ __forceinline__ float rescaled(float sum, float factor) { return __builtin_isfinite(sum) ? sum * factor : sum; }
 
 // For sched_barrier: vector and scalar arithmetic may cross, matrix and LDS instructions stay in order.
 constexpr int kAluMayCross = 0x2 | 0x4;
@@ -540,7 +544,7 @@ __device__ __forceinline__ void join_shares(const Shape& s, const Chunk& ck, con
         for (int i = 0; i < kMaxShares; ++i) {
             if (i < n) {
                 const float sc = fast_exp2(ml[r * kMaxShares + i] - mu);
-                num += sc * a[i];
+                num += rescaled(a[i], sc);
                 den += sc * ml[(ROWS + r) * kMaxShares + i];
             }
         }
@@ -614,9 +618,9 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
 
     // the new rows, a block of their own for the wave that would take the next one: to the pages, and attended as
     // the pages hold them
+    bool odd = false;  // a new value that is not finite
     if (last_share && wave == (blocks & 3)) {
         const int cc = lane % CPR;
-        bool odd = false;
         for (int i0 = 0; i0 < KB; i0 += 64 / CPR) {
             const int i = i0 + lane / CPR;
             u32x4 kr = {0u, 0u, 0u, 0u}, vr = {0u, 0u, 0u, 0u};
@@ -669,7 +673,6 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
         }
         asm volatile("" ::: "memory");
         qr.template step<true>(kst, vst, scales, f, f + c, s.scale2);
-        if (__builtin_amdgcn_ballot_w64(odd) != 0) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, f, f + c);
         asm volatile("" ::: "memory");
     }
     for (; n0 < t1; n0 += 4 * KB) {
@@ -686,6 +689,7 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
         else qr.template step<true>(kst, vst, scales, n0, t1, s.scale2);
     }
     qr.close();
+    if (__builtin_amdgcn_ballot_w64(odd) != 0) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, f, f + c);
 
     // the waves' partials through LDS
     __syncthreads();  // every wave is done with its stage
@@ -717,7 +721,7 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float sc = fast_exp2(wm[w * ROWS + r] - mu);
-            num += sc * wacc[(size_t)(w * ROWS + r) * D + e];
+            num += rescaled(wacc[(size_t)(w * ROWS + r) * D + e], sc);
             den += sc * wl[w * ROWS + r];
         }
         if (it.shares == 1) {

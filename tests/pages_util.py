@@ -242,3 +242,31 @@ def check(c, out_bf16=False, **kw):
     assert np.all(err <= tol), f"{np.count_nonzero(~(err <= tol))} of {err.size} off; worst {np.nanmax(err / tol):.2f} of the bound"
     c["pool"].check(pool)
     return out, pool
+
+
+def set_value(c, which, i, n, dims, b):
+    """Elements `dims` of row n of segment i, every KV head, in a bf16 pool or, for a new token's row, its input."""
+    f, m = parts(c)[i]
+    if n < f:
+        c["pool"].x[which][c["table"][i][n // c["page"]], :, n % c["page"], dims] = b
+    else:
+        c[("k_new", "v_new")[which]].reshape(c["B"] * c["L"], c["chunk"], c["hkv"], c["d"])[i, n - f, :, dims] = b
+
+
+def check_all(c, out_bf16=False, **kw):
+    """check() where results may be infinities and NaN: these have to be where the 64-bit form has them."""
+    out, pool = call(c, out_bf16, **kw)
+    with np.errstate(invalid="ignore"):
+        want, mag, qk = reference(c)
+        rows = np.zeros((c["B"] * c["L"], c["chunk"]), bool)  # the rows that the call writes
+        for i, (f, n) in enumerate(parts(c)):
+            rows[i, :n] = True
+        rows = rows.reshape(c["B"], c["L"], c["chunk"])
+        got, want, mag, qk = (x[rows] for x in (out, want, mag, qk))
+        odd = ~np.isfinite(want)
+        assert np.array_equal(got[odd], want[odd], equal_nan=True), \
+            f"{np.count_nonzero(~((got == want) | (np.isnan(got) & np.isnan(want)))[odd])} of {odd.sum()} non-finite results differ"
+        # a finite result of a row with non-finite ones: its own dim's magnitudes
+        err, tol = np.abs(got - want)[~odd], np.broadcast_to(tolerance(c, want, mag, qk, out_bf16), got.shape)[~odd]
+        assert np.all(err <= tol), f"{np.count_nonzero(~(err <= tol))} of {err.size} finite results off"
+    c["pool"].check(pool)

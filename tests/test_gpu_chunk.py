@@ -158,6 +158,45 @@ def test_bad_retained_rows(lib, kind, chunk, where):
     assert np.all((np.abs(out - want) <= tolerance(c, want, mag, qk, False))[1])
 
 
+# (query heads, KV heads, chunk): few query rows (16 and 32), 64-row tiles, two 128-row tiles
+SHAPES = [(2, 2, 1), (2, 2, 4), (14, 2, 4), (2, 2, 40), (6, 2, 70)]
+
+
+def _odd_values(c, rows, low):
+    """Infinities and NaN in the values of `rows` of every segment: one sign, both signs, a NaN beside an infinity, in dims
+    of their own.  low: these rows' logits lie 150 (natural units) below the others', a probability of e^-150, which is 0
+    in 32 bits."""
+    from tests.pages_util import bits, set_value
+    q = bits(np.sqrt(c["d"]))
+    if low:
+        c["q"][:] = 0
+        c["q"][..., 0] = q
+    for i, (f, m) in enumerate(parts(c)):
+        for r in range(f + m) if low else []:
+            set_value(c, 0, i, r, slice(0, 1), bits(2.0))
+        here = [r for r in rows(f, m) if 0 <= r < f + m]
+        for x, r in enumerate(here):
+            if low:
+                set_value(c, 0, i, r, slice(0, 1), bits(-148.0))
+            set_value(c, 1, i, r, slice(3, 4), bits(np.inf))
+            set_value(c, 1, i, r, slice(40, 41), bits(-np.inf))
+            set_value(c, 1, i, r, slice(17, 18), bits(-np.inf if x % 2 else np.inf))
+            set_value(c, 1, i, r, slice(c["d"] - 1, c["d"]), bits(np.nan if x == 0 else np.inf))
+
+
+@pytest.mark.parametrize("hq,hkv,chunk", SHAPES)
+@pytest.mark.parametrize("low", [False, True])
+@pytest.mark.parametrize("out_bf16", [False, True])
+def test_infinite_new_values(lib, hq, hkv, chunk, low, out_bf16):
+    """An infinity in a new token's value is the result's infinity, however small its probability: in segments of no,
+    few and many retained rows (shares), for the tokens that see it and no other."""
+    from tests.pages_util import check_all
+    log(f"infinite new values hq={hq} hkv={hkv} chunk={chunk} low={low} bf16={out_bf16}")
+    c = case(60 + chunk, 2, 2, hq, hkv, 64, chunk, bd.CACHE_BF16, 16, [0, 70, 1500, 33], [0, 2], None, chunk + 2)
+    _odd_values(c, lambda f, m: [f + m // 2, f + m - 1], low)
+    check_all(c, out_bf16)
+
+
 def test_extreme_logits(lib):
     """Logits far apart (one key takes all), equal, and so low that a key of probability 0 has a value of 1e38."""
     from tests.pages_util import bits
