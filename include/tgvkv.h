@@ -434,7 +434,9 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
  * f = budgets[b*L+l] + steps[b], it writes k_new / v_new of token i at row f + i of its pages, quantised
  * with an 8-bit kind, and computes for each query head h
  *   out[b][l][i][h] = softmax_n(tau q[b][l][i][h] . K[n]) V[n],  n <= f + i,
- * over the rows as the pages hold them (Eq. (2)-(4); c decode steps in one call).
+ * over the rows as the pages hold them (Eq. (2)-(4); c decode steps in one call).  An infinity in a row of bf16 V counts
+ * as one however small its probability: the dim's result is that infinity, or a NaN with both signs or a NaN among the
+ * rows that the token sees.
  * A sequence takes no part, and its pages and rows of out are not touched, unless steps[b] >= 0,
  * 1 <= c <= chunk and steps[b] + c <= decode_reserve; nor does a segment whose table row is too narrow
  * for its f + c rows.  Tokens i >= c of the inputs are not read and their rows of out not touched.  A new

@@ -29,6 +29,8 @@
 // A value that is not finite in a new token's V would reach earlier tokens through 0 * inf; such elements
 // are staged as 0 and added to the rows that see them at the end (rare: one flag is looked at), after the last
 // rescaling: a factor or a probability too small for 32 bits times an infinity is a NaN, where the sum is infinite.
+// Those of retained rows, which all of the chunk's rows see, are looked for only where a sum came out not finite,
+// and take its place: an infinity counts as one whatever its probability.
 #include <algorithm>
 #include <atomic>
 #include <chrono>
@@ -332,6 +334,71 @@ struct QueryRows {
     __device__ __forceinline__ void close() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) l[nt] = sum_xor32(sum_xor16(l[nt]));
+    }
+
+    // Whether a weighted sum of the wave is not finite: 0 times it is a NaN then.
+    __device__ __forceinline__ bool any_non_finite() const {
+        float x = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x = __builtin_fmaf(o[nt][db][j], 0.f, x);
+        return __builtin_amdgcn_ballot_w64(x != x) != 0;
+    }
+
+    // With bf16 pages: the sums over rows that hold an infinity or a NaN, from the blocks of 32 rows n_beg, n_beg + step ..
+    // below n_end.  Every query row sees these rows, so such a dim's sum is that of its non-finite values, where the
+    // products made a NaN of every infinity (its probability's lower parts are 0 or negative, and a row that repeats the last
+    // has the probability 0).  Only called where a sum is not finite, which is rare.
+    __device__ __forceinline__ void sum_non_finite(const Pages& pg, const PageRows& pages, int n_beg, int n_end, int step) {
+        constexpr int CH = D / 8, N = 32 * CH / 64;  // 16-byte pieces per row, and of 32 rows per lane
+        const int lane = threadIdx.x & 63, qq = lane >> 4;
+        uint32_t dims = 0;  // bit 4 db + j
+        static_assert(D / 4 <= 32, "a bit for each of the lane's dims");
+#pragma unroll 1
+        for (uint32_t add = 0;; add = ~0u) {
+#pragma unroll 1
+            for (int n0 = n_beg; n0 < n_end; n0 += step) {
+                bool here = false;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const size_t row = pages.row(min(n0 + (i * 64 + lane) / CH, n_end - 1));
+                    here |= non_finite(load16(pg.v + (row * D + lane % CH * 8) * 2));
+                }
+                if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+#pragma unroll 1
+                for (int n = n0; n < min(n0 + 32, n_end); ++n) {
+                    const uint8_t* v = pg.v + (pages.row(n) * D + 4 * qq) * 2;
+#pragma unroll
+                    for (int db = 0; db < D / 16; ++db) {
+                        const u32x2 w = *reinterpret_cast<const u32x2*>(v + 32 * db);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t x = j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16;
+                            // masks in vector registers: 32 conditions in scalar ones spill
+                            const uint32_t odd = (x & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
+                            dims |= odd & 1u << (4 * db + j);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) o[nt][db][j] += __uint_as_float(x & odd & add);
+                        }
+                    }
+                }
+            }
+            if (add != 0) return;
+            if (__builtin_amdgcn_ballot_w64(dims != 0) == 0) return;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint32_t drop = (uint32_t)((int)(dims << (31 - 4 * db - j)) >> 31);
+                        o[nt][db][j] = __uint_as_float(__float_as_uint(o[nt][db][j]) & ~drop);
+                    }
+            }
+        }
     }
 
     // Adds the non-finite values of V rows n0 .. n1 - 1 that a row sees: those of the new tokens in bf16, or, with
@@ -689,6 +756,9 @@ __global__ __launch_bounds__(kThreads, KIND != kCacheBf16 && NT == 1 ? 3 : 2) vo
         else qr.template step<true>(kst, vst, scales, n0, t1, s.scale2);
     }
     qr.close();
+    if constexpr (!CODES) {
+        if (qr.any_non_finite()) qr.sum_non_finite(pg, pages, t0 + KB * wave, t1, 4 * KB);
+    }
     if (__builtin_amdgcn_ballot_w64(odd) != 0) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, f, f + c);
 
     // the waves' partials through LDS
@@ -885,6 +955,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
         qr.weigh(a[2], a[3], smem + KT * B::K + 32 * B::V, nullptr, s.scale2);
     }
     qr.close();
+    if constexpr (KIND == kCacheBf16) {
+        if (qr.any_non_finite()) qr.sum_non_finite(pg, pages, t0, min(t1, f), 32);
+    }
     __syncthreads();
     if (odd_seen) qr.template add_non_finite<KIND>(s, ck, part, bl, kvh, max(f, t0), t1);
 

@@ -197,6 +197,49 @@ def test_infinite_new_values(lib, hq, hkv, chunk, low, out_bf16):
     check_all(c, out_bf16)
 
 
+@pytest.mark.parametrize("hq,hkv,chunk", SHAPES)
+@pytest.mark.parametrize("low", [False, True])
+@pytest.mark.parametrize("out_bf16", [False, True])
+@pytest.mark.parametrize("where", ["first", "last", "scattered"])
+def test_infinite_retained_values(lib, hq, hkv, chunk, low, out_bf16, where):
+    """The same in retained rows, and in retained and new ones together: in the first block and in the last one, which
+    ends inside a block, in every wave's blocks and in shares."""
+    from tests.pages_util import check_all
+    log(f"infinite retained values hq={hq} hkv={hkv} chunk={chunk} low={low} bf16={out_bf16} {where}")
+    c = case(70 + chunk, 2, 2, hq, hkv, 128, chunk, bd.CACHE_BF16, 16, [1, 75, 1500, 33], [0, 2], None, chunk + 2)
+    rows = dict(first=lambda f, m: [0, 5], last=lambda f, m: [f - 1], scattered=lambda f, m: [7, 31, 32, f // 2, 700, f - 3, f + m // 2])
+    _odd_values(c, rows[where], low)
+    check_all(c, out_bf16)
+
+
+def test_infinite_values_one_by_one(lib):
+    """Tokens whose values are infinite as one chunk and one by one, by extend and by decode: the same infinities."""
+    import torch
+    log("infinite values one by one")
+    from tests.pages_util import bits
+    c = case(80, 2, 2, 2, 2, 64, 3, bd.CACHE_BF16, 16, [40, 7, 300, 0], [0, 1], None, 8)
+    for t, e, x in ((0, 4, np.inf), (1, 9, -np.inf), (2, 4, np.inf), (2, 9, np.inf), (1, 33, np.nan)):
+        c["v_new"][:, :, t, :, e] = bits(x)
+    whole, _ = call(c)
+    assert np.all(whole[..., 4] == np.inf) and np.all(whole[:, :, 1, :, 9] == -np.inf) and np.all(np.isnan(whole[:, :, 2, :, 9]))
+    odd = ~np.isfinite(whole)
+    extend, decode = c["pool"].device(), c["pool"].device()
+    p = bd.make_problem(2, 2, 2, 2, 64, 1, 0, 0)
+    ws = torch.zeros(max(1, bd.workspace_size(p, None, bd.CALL_DECODE)), dtype=torch.uint8, device="cuda")
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    b16 = lambda a: up(a.view(np.int16)).view(torch.bfloat16)  # noqa: E731
+    for t in range(3):
+        s = dict(c, chunk=1, steps=c["steps"] + t, **{n: np.ascontiguousarray(c[n][:, :, t:t + 1]) for n in ("q", "k_new", "v_new")})
+        got, _ = call(s, pool=extend)
+        out = torch.empty(2, 2, 2, 64, device="cuda")
+        decode.decode(p, None, up(c["table"]), up(c["budgets"]), 8, up(s["steps"]), *(b16(s[n][:, :, 0]) for n in ("q", "k_new", "v_new")),
+                      out, ws)
+        torch.cuda.synchronize()
+        want, here = whole[:, :, t], odd[:, :, t]
+        for x in (got[:, :, 0], out.double().cpu().numpy()):
+            assert np.array_equal(x[here], want[here], equal_nan=True) and np.all(np.isfinite(x[~here])), t
+
+
 def test_extreme_logits(lib):
     """Logits far apart (one key takes all), equal, and so low that a key of probability 0 has a value of 1e38."""
     from tests.pages_util import bits
