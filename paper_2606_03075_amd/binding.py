@@ -445,14 +445,26 @@ def chunk_workspace_size(problem, opts, chunk) -> int:
     return int(load_library().tgvkv_chunk_workspace_size(ctypes.byref(problem), _opts_ref(opts), int(chunk)))
 
 
+def _room(t, kind, n, device, name):
+    """_at of a tensor of at least n elements (or no tensor)."""
+    if t is not None and isinstance(t, _torch.Tensor) and t.numel() < n:
+        raise ValueError(f"{name} must hold {n} elements")
+    return _at(t, kind, None, device, name)
+
+
 def _store(fn, problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream, unit_order):
     desc, device = _pages(pool, problem.heads_kv, problem.head_dim)
+    width, segments, per_head, kept = _table_width(block_table, problem), problem.batch * problem.layers, 1, int(total_budget)
+    rows = segments * problem.heads_kv * (problem.n_sys + problem.n_vis + problem.n_qst) * problem.head_dim
+    if opts is not None:
+        per_head = problem.heads_kv if opts.head_mode == 1 else 1
+        kept = kept_per_sequence(problem, opts, total_budget) if opts.vision_only else kept  # with the text of every layer
     st = getattr(load_library(), fn)(
-        ctypes.byref(problem), _opts_ref(opts), _at(k, _BF16, None, device, "k"), _at(v, _BF16, None, device, "v"),
-        _at(idx, _I32, None, device, "idx"), _at(budgets, _I32, None, device, "budgets"),
-        _at(idx_offsets, _I64, None, device, "idx_offsets"), int(total_budget), ctypes.byref(desc),
-        _at(block_table, _I32, None, device, "block_table"), _table_width(block_table, problem),
-        _at(unit_order, _I32, None, device, "unit_order"), _stream_on(stream, device))
+        ctypes.byref(problem), _opts_ref(opts), _room(k, _BF16, rows, device, "k"), _room(v, _BF16, rows, device, "v"),
+        _room(idx, _I32, problem.batch * kept * per_head, device, "idx"), _room(budgets, _I32, segments, device, "budgets"),
+        _room(idx_offsets, _I64, segments + 1, device, "idx_offsets"), int(total_budget), ctypes.byref(desc),
+        _at(block_table, _I32, None, device, "block_table"), width,
+        _room(unit_order, _I32, segments, device, "unit_order"), _stream_on(stream, device))
     _check(fn, st)
 
 

@@ -122,6 +122,46 @@ def test_a_store_takes_a_table_of_any_width(so):
     assert store(problem=P(batch=0), pool=pages(k=None)) == 0
 
 
+def test_stores_check_their_tensors_sizes(so, monkeypatch):
+    """A tensor too small for the problem is refused before the call, which reads by the problem's sizes: a short `budgets`
+    or `idx` would be read out of range on the GPU.  (Host tensors, taken for the GPU's; the library's calls only count.)"""
+    import torch
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+    real = bd.load_library()
+    Library.tgvkv_sizes = staticmethod(lambda *a: real.tgvkv_sizes(*a))
+    monkeypatch.setattr(bd, "load_library", lambda path=None: Library())
+    monkeypatch.setattr(bd, "_pages", lambda pool, hkv, d: (bd.TgvkvPages(), -1))  # host tensors' device number
+    monkeypatch.setattr(bd, "_stream_on", lambda stream, device: 0)
+    bd._import_torch()
+    zeros = lambda n, dtype: torch.zeros(n, dtype=dtype)  # noqa: E731
+    B, L, hkv, N, d = 2, 3, 2, 48, 64
+    for head_mode, vision_only, kept in ((0, False, 90), (1, False, 90), (0, True, 90 + 3 * 8)):
+        p, o = P(batch=B, layers=L, heads_kv=hkv, head_dim=d), bd.make_opts(head_mode=head_mode, vision_only=vision_only)
+        good = dict(k=zeros(B * L * hkv * N * d, torch.bfloat16), v=zeros(B * L * hkv * N * d, torch.bfloat16),
+                    idx=zeros(B * kept * (hkv if head_mode else 1), torch.int32), budgets=zeros(B * L, torch.int32),
+                    idx_offsets=zeros(B * L + 1, torch.int64), table=zeros((B * L, 6), torch.int32),
+                    unit_order=zeros(B * L, torch.int32))
+
+        def go(call, **kw):
+            a = dict(good, **kw)
+            call(p, o, a["k"], a["v"], a["idx"], a["budgets"], a["idx_offsets"], 90, None, a["table"], unit_order=a["unit_order"])
+        for call in (bd.tgvkv_compact_pages, bd.tgvkv_store_pages):
+            del calls[:]
+            go(call)
+            go(call, unit_order=None, idx=torch.cat([good["idx"], good["idx"]]))  # room to spare
+            assert calls == [call.__name__] * 2
+            for name in ("k", "v", "idx", "budgets", "idx_offsets", "unit_order"):
+                with pytest.raises(ValueError, match=name):
+                    go(call, **{name: good[name][:-1].contiguous()})
+            with pytest.raises(ValueError):
+                go(call, table=good["table"][1:].contiguous())
+            assert len(calls) == 2
+
+
 def test_chunk_workspace_size(so):
     assert bd.chunk_workspace_size(P(head_dim=96), None, 1) == 0
     assert bd.chunk_workspace_size(P(), None, 0) == 0
