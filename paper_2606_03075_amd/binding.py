@@ -669,11 +669,28 @@ class PagedPool:
         self.free = list(range(n_pages))
         self.device = device
 
-    def attach(self, k_pool, v_pool, k_exp=None, v_exp=None):
-        """Serve from the caller's pool tensors (same page size and kind) instead of the pool's own."""
+    def attach(self, k_pool, v_pool, k_exp=None, v_exp=None, free=()):
+        """Serve from the caller's pool tensors (the same heads, page size, head dim and kind, any number of pages)
+        instead of the pool's own.  free: the ids of the pages that none of the caller's tables uses, which admit()
+        takes from; none by default."""
+        if _torch is None:
+            _import_torch()
+        n = k_pool.shape[0] if isinstance(k_pool, _torch.Tensor) and k_pool.dim() == 4 else 0
+        shape, held = (n, *self.k_pool.shape[1:]), _KINDS[(_BF16, _FP8, _INT8)[self.kind]]
+        wanted = [("k_pool", k_pool, shape, held), ("v_pool", v_pool, shape, held)]
+        if self.kind != CACHE_BF16:
+            wanted += [("k_exp", k_exp, shape[:3], _KINDS[_U8]), ("v_exp", v_exp, shape[:3], _KINDS[_U8])]
+        elif k_exp is not None or v_exp is not None:
+            raise ValueError("bf16 pages have no exponent bytes")
+        for name, t, size, dtypes in wanted:
+            if n < 1 or not isinstance(t, _torch.Tensor) or t.shape != size or t.dtype not in dtypes or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtypes[0]} tensor of the pool's layout, [n_pages, "
+                                 f"{', '.join(map(str, size[1:]))}]")
+        free = [int(i) for i in free]
+        if len(set(free)) < len(free) or any(i < 0 or i >= n for i in free):
+            raise ValueError("free must be distinct page ids below n_pages")
         self.k_pool, self.v_pool, self.k_exp, self.v_exp = k_pool, v_pool, k_exp, v_exp
-        self.n_pages = int(k_pool.shape[0])
-        self.free = list(range(self.n_pages))
+        self.n_pages, self.free = int(n), free
 
     def admit(self, buf: "EvictionBuffers", k, v, stream=None):
         """Page table [B*L, max_pages] of an evicted batch, with its rows compacted into the pool."""

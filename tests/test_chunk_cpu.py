@@ -162,6 +162,41 @@ def test_stores_check_their_tensors_sizes(so, monkeypatch):
             assert len(calls) == 2
 
 
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_attached_pools_are_checked(kind):
+    """attach() takes only tensors of the pool's own layout and kind, and leaves the pool as it was otherwise; no page is
+    free for admit() but those that the caller names, for its tables may use any."""
+    import torch
+    dtype = (torch.bfloat16, torch.float8_e4m3fn, torch.int8)[kind]
+    make = lambda n, hkv=2, page=8, d=64, t=dtype: torch.empty(n, hkv, page, d, dtype=t)  # noqa: E731
+    exps = lambda n, hkv=2, page=8, t=torch.uint8: None if kind == 0 else torch.zeros(n, hkv, page, dtype=t)  # noqa: E731
+    pool = bd.PagedPool(2, 64, 8, 3, device="cpu", kind=kind)
+    assert pool.free == [0, 1, 2]
+    before = (pool.k_pool, pool.v_pool, pool.k_exp, pool.v_exp)
+    k, v, ke, ve = make(5), make(5), exps(5), exps(5)
+    bad = [(make(5, hkv=3), v, ke, ve), (k, make(4), ke, ve), (make(5, page=16), make(5, page=16), ke, ve),
+           (make(5, d=128), make(5, d=128), ke, ve), (k.view(torch.uint8), v, ke, ve), (k, None, ke, ve), (None, v, ke, ve),
+           (make(10)[::2], v, ke, ve), (k, v.transpose(0, 1), ke, ve), (make(0), make(0), exps(0), exps(0)), (k[0], v[0], ke, ve)]
+    if kind:
+        bad += [(k, v, None, ve), (k, v, ke, exps(4)), (k, v, ke.to(torch.int8), ve), (k, v, ke, exps(10)[::2])]
+    else:
+        bad += [(k, v, torch.zeros(5, 2, 8, dtype=torch.uint8), None)]
+    for args in bad:
+        with pytest.raises((ValueError, TypeError)):
+            pool.attach(*args)
+    for free in ([5], [-1], [1, 2, 1]):
+        with pytest.raises(ValueError):
+            pool.attach(k, v, ke, ve, free=free)
+    assert all(a is b for a, b in zip(before, (pool.k_pool, pool.v_pool, pool.k_exp, pool.v_exp)))
+    assert pool.free == [0, 1, 2] and pool.n_pages == 3
+    pool.attach(k, v, ke, ve)
+    assert pool.free == [] and pool.n_pages == 5 and pool.k_pool is k and pool.v_exp is ve
+    pool.attach(k, v, ke, ve, free=range(2, 5))
+    assert pool.free == [2, 3, 4]
+    pool.release(torch.tensor([[0, 1, -1]], dtype=torch.int32))
+    assert pool.free == [2, 3, 4, 0, 1]
+
+
 def test_chunk_workspace_size(so):
     assert bd.chunk_workspace_size(P(head_dim=96), None, 1) == 0
     assert bd.chunk_workspace_size(P(), None, 0) == 0
