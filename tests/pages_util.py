@@ -270,3 +270,45 @@ def check_all(c, out_bf16=False, **kw):
         err, tol = np.abs(got - want)[~odd], np.broadcast_to(tolerance(c, want, mag, qk, out_bf16), got.shape)[~odd]
         assert np.all(err <= tol), f"{np.count_nonzero(~(err <= tol))} of {err.size} finite results off"
     c["pool"].check(pool)
+
+
+# How far the products with V may change a probability.  In the inputs of one_term_case() a logit is one product (its sum
+# exact), a result one probability over the common sum, and the results' shares of their total free of that sum's errors.
+# A share is off by twice the following, relative to itself, with probabilities of all their 24 bits:
+#   2^-21 ln 2   the exponent, in [8, 16) below the reference: one rounding of an fma
+#   3 2^-24      the logit's scale: sm_scale, log2 e and their product rounded, times at most 1.5 (base 2) and ln 2
+#   3 2^-23      exp2 of the exponent and of the factors that join waves and shares, one unit in the last place each
+#   3 2^-24      the two joins' products and the division or the product with the reciprocal
+# A probability in two bf16 parts is off by up to 2^-18 of itself.
+ONE_TERM_BOUND = 2 * (2.0 ** -21 * np.log(2) + (3 * 1.5 * np.log(2) + 3 * 2 + 3) * 2.0 ** -24)
+
+
+def one_term_case(seed, hq, hkv, d, chunk, kind, rows, page=16):
+    """One segment of `rows` retained rows and `chunk` new ones, in which every key and query is one value in dim 0, and
+    every dim of V one 1 in a row of its own; (case, the dims' rows)."""
+    rng = np.random.default_rng(seed)
+    c = case(seed, 1, 1, hq, hkv, d, chunk, kind, page, [0], [rows], None, rows + chunk, order=False)
+    at = rng.choice(rows, d, replace=False)
+    x = np.zeros((2, rows + chunk, hkv, d), np.float32)
+    x[0, ..., 0] = rng.uniform(0, 8, (rows + chunk, hkv))
+    x[1, at, :, np.arange(d)] = 1.0
+    for w in range(2):
+        for n in range(rows):
+            c["pool"].write(w, c["table"][0], n, bits(x[w, n]))
+        c[("k_new", "v_new")[w]][0, 0] = bits(x[w, rows:])
+    c["q"][:] = 0
+    c["q"][..., 0] = bits(1.0)
+    return c, at
+
+
+def one_term_shares(c, at):
+    """(results' shares of their total, the total), [chunk, hq, d] and [chunk, hq], in 64 bits; to be called after the call."""
+    reference_pool, (f, m) = c["pool"], parts(c)[0]
+    for r in range(m):
+        reference_pool.write(0, c["table"][0], f + r, c["k_new"][0, 0, r])
+    z = reference_pool.rows(0, c["table"][0], 0, f + m)[..., 0] / np.sqrt(c["d"])  # [hkv][rows]
+    p = np.exp(z)[np.arange(c["hq"]) // (c["hq"] // c["hkv"])]  # [hq][rows]
+    sums = np.cumsum(p, 1)[:, f:].T  # over the rows that token i sees
+    mine = p[:, at]
+    total = mine.sum(1)
+    return np.broadcast_to(mine / total[:, None], (m, *mine.shape)), total[None] / sums

@@ -239,6 +239,34 @@ def test_an_older_library_is_refused(tmp_path):
         bd.load_library(str(lib))
 
 
+def test_one_term_bound_tells_two_parts_from_three():
+    """The arithmetic of the products with V in float32: probabilities in three bf16 parts stay below the bound that the
+    GPU tests hold the kernels to, in two parts they do not."""
+    from tests.pages_util import ONE_TERM_BOUND
+    f32 = np.float32
+
+    def parts_of(p, n):
+        out = np.zeros_like(p)
+        for _ in range(n):
+            b = bf16_bits_to_f32(bits(p))
+            out, p = out + b, p - b
+        return out.astype(np.float64)
+    rng = np.random.default_rng(0)
+    worst = {2: [], 3: []}
+    for d in (64, 128):
+        for _ in range(20):
+            a = bf16_bits_to_f32(bits(rng.uniform(0, 8, (4, d))))
+            want = np.exp(a.astype(np.float64) / np.sqrt(d))
+            want /= want.sum(1, keepdims=True)
+            scale2 = f32(f32(1) / np.sqrt(f32(d))) * f32(1.4426950408889634)
+            ref = (a * scale2).max(1, keepdims=True) + f32(8)
+            p = np.exp2((a * scale2 - ref).astype(np.float64)).astype(f32)
+            for n in worst:
+                x = parts_of(p, n)
+                worst[n].append(np.abs(x / x.sum(1, keepdims=True) / want - 1).max())
+    assert max(worst[3]) <= ONE_TERM_BOUND < min(worst[2])
+
+
 def test_plain_quantiser():
     """The grid is e4m3's (torch's cast agrees on every code), the exponent is the least that fits, a row of its own
     values is left as it is."""

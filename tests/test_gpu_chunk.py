@@ -158,6 +158,25 @@ def test_bad_retained_rows(lib, kind, chunk, where):
     assert np.all((np.abs(out - want) <= tolerance(c, want, mag, qk, False))[1])
 
 
+@pytest.mark.parametrize("hq,hkv,d,chunk", [(4, 4, 64, 1), (8, 2, 128, 4), (7, 1, 64, 4), (2, 2, 128, 40), (3, 1, 64, 30), (4, 2, 128, 70)])
+@pytest.mark.parametrize("kind,rows", [(bd.CACHE_BF16, 130), (bd.CACHE_BF16, 700), (bd.CACHE_BF16, 6001), (bd.CACHE_FP8, 500),
+                                       (bd.CACHE_INT8, 500)])
+def test_probabilities_of_24_bits(lib, hq, hkv, d, chunk, kind, rows):
+    """32-bit results take the probabilities whole: results that are one probability each, across waves and shares, are
+    off by less than a probability in two bf16 parts would be."""
+    from tests.pages_util import ONE_TERM_BOUND, one_term_case, one_term_shares
+    log(f"24 bits hq={hq} hkv={hkv} d={d} chunk={chunk} kind={kind} rows={rows}")
+    c, at = one_term_case(rows + chunk, hq, hkv, d, chunk, kind, rows)
+    out = call(c)[0][0, 0]
+    want, total = one_term_shares(c, at)
+    got = out.sum(-1)
+    off = np.abs(out / got[..., None] / want - 1).max()
+    print(f"    off by {off:.2e}")
+    assert off <= ONE_TERM_BOUND
+    # the sum of the probabilities: a lane adds a quarter of the rows at most, one rounding each, and the joins
+    assert np.abs(got / total - 1).max() <= ONE_TERM_BOUND + ((rows + chunk) / 4 + 40) * 2.0 ** -24
+
+
 # (query heads, KV heads, chunk): few query rows (16 and 32), 64-row tiles, two 128-row tiles
 SHAPES = [(2, 2, 1), (2, 2, 4), (14, 2, 4), (2, 2, 40), (6, 2, 70)]
 
