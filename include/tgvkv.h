@@ -65,7 +65,9 @@ typedef enum tgvkv_status {
  * (TGVKV_E_UNSUPPORTED beyond them): layers <= 512, N <= 2^24,
  * heads_q / heads_kv <= 16, and the text rows one KV head scores,
  * (heads_q / heads_kv) * (n_sys + n_qst), at most 16384.  heads_q must be a
- * multiple of heads_kv; every count is >= 0 and N >= 1 (TGVKV_E_INVAL). */
+ * multiple of heads_kv; every count is >= 0 and N >= 1 (TGVKV_E_INVAL).  Compaction, decode
+ * and the calls on pages take batch * layers * heads_kv < 2^24 (reads < 2^26): a launch's
+ * threads are numbered in 32 bits (TGVKV_E_UNSUPPORTED). */
 typedef struct tgvkv_problem {
     int32_t batch;
     int32_t layers;
@@ -447,7 +449,9 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
  * steps, n_new_or_null  int32 [B], device
  * out          [B][L][chunk][heads_q][head_dim], f32, or bf16 with out_bf16 != 0 (the probabilities then enter
  *              the product with the values in bf16 too, not in three bf16 parts)
- * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1 (TGVKV_E_UNSUPPORTED).
+ * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1, and fewer than 2^24 workgroups, one per
+ * segment and KV head and, above 32 query rows chunk * heads_q / heads_kv, per 64 or (above 64) 128 of these
+ * (TGVKV_E_UNSUPPORTED).
  * workspace >= tgvkv_chunk_workspace_size(p, o, chunk) (may be 0 bytes; TGVKV_E_WORKSPACE if it is less than this
  * chunk needs), with any first contents; calls that
  * may overlap need a workspace each.  unit_order_or_null as for tgvkv_decode_attn. */

@@ -22,6 +22,8 @@ constexpr int64_t kMaxTokens = int64_t(1) << 24;
 constexpr int64_t kMaxTextRowsPerKvHead = 16384;  // LDS row-normaliser buffer of the text pass
 constexpr int32_t kMaxGroup = 16;                  // query heads per KV head (decode registers)
 constexpr int64_t kMaxBlocks = (int64_t(1) << 31) - 1;
+// Workgroups of 256 threads in a launch, whose threads are numbered in 32 bits: of more only a part runs, without an error.
+constexpr int64_t kMaxWorkgroups = (int64_t(1) << 24) - 1;
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -188,6 +190,11 @@ bool chunk_fits(const Shape& s, int32_t chunk) {
     return chunk >= 1 && (int64_t)s.B * s.L * s.H <= kMaxBlocks / chunk;
 }
 
+// Whether a launch of a workgroup of `threads` per (sequence, layer, KV head) numbers them all.
+bool units_fit(const Shape& s, int threads = 256) {
+    return (int64_t)s.B * s.L * s.Hkv <= ((kMaxWorkgroups + 1) * 256 - 1) / threads;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The pool's and the table's memory, needed by every call that has work to do.
@@ -223,7 +230,7 @@ tgvkv_status store_pages(const tgvkv_problem* problem, const tgvkv_opts* opts, c
         !pages_present(pg))
         return TGVKV_E_INVAL;
     if (!aligned16(k) || !aligned16(v)) return TGVKV_E_INVAL;
-    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     return hip_status(tgvkv::launch_compact_pages(s, pg, static_cast<const uint16_t*>(k),
                                                   static_cast<const uint16_t*>(v), idx, budgets, idx_offsets,
                                                   (int64_t)s.B * kept, unit_order, stream));
@@ -369,7 +376,7 @@ tgvkv_status tgvkv_compact(const tgvkv_problem* problem, const tgvkv_opts* opts,
         return TGVKV_E_INVAL;
     if (!aligned16(k) || !aligned16(v) || !aligned16(kc) || !aligned16(vc)) return TGVKV_E_INVAL;
     const int64_t rows = (int64_t)s.B * kept;
-    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     return hip_status(tgvkv::launch_compact(s, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), idx,
                                             budgets, idx_offsets, seg_offsets, decode_reserve, rows,
                                             unit_order_or_null, static_cast<uint16_t*>(kc),
@@ -392,6 +399,7 @@ tgvkv_status tgvkv_decode_attn(const tgvkv_problem* problem, const tgvkv_opts* o
         return TGVKV_E_INVAL;
     if (!aligned16(kc) || !aligned16(vc) || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new))
         return TGVKV_E_INVAL;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     const size_t need = decode_workspace_bytes(s);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return TGVKV_E_WORKSPACE;
     return hip_status(tgvkv::launch_decode(s, static_cast<uint16_t*>(kc), static_cast<uint16_t*>(vc), budgets,
@@ -415,6 +423,7 @@ tgvkv_status tgvkv_decode_attn_noalloc(const tgvkv_problem* problem, const tgvkv
         return TGVKV_E_INVAL;
     if (!aligned16(kc) || !aligned16(vc) || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new))
         return TGVKV_E_INVAL;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     const size_t need = decode_workspace_bytes(s);
     if (need > tgvkv::kDecodeScratchBytes) return TGVKV_E_WORKSPACE;
     float* ws = nullptr;
@@ -498,7 +507,7 @@ tgvkv_status tgvkv_compact_paged(const tgvkv_problem* problem, const tgvkv_opts*
         block_table == nullptr || k_pool == nullptr || v_pool == nullptr)
         return TGVKV_E_INVAL;
     if (!aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool)) return TGVKV_E_INVAL;
-    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     return hip_status(tgvkv::launch_compact_paged(
         s, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), idx, budgets, idx_offsets,
         (int64_t)s.B * kept, block_table, max_pages, sh, n_pages, unit_order_or_null, static_cast<uint16_t*>(k_pool),
@@ -523,6 +532,7 @@ tgvkv_status tgvkv_decode_attn_paged(const tgvkv_problem* problem, const tgvkv_o
         return TGVKV_E_INVAL;
     if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new))
         return TGVKV_E_INVAL;
+    if (!units_fit(s)) return TGVKV_E_UNSUPPORTED;
     const size_t need = decode_workspace_bytes(s);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return TGVKV_E_WORKSPACE;
     return hip_status(tgvkv::launch_decode_paged(
@@ -562,7 +572,7 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
     if (!pages_present(pg) || count == nullptr || seg_offsets == nullptr || k_out == nullptr || v_out == nullptr)
         return TGVKV_E_INVAL;
     if (!aligned16(k_out) || !aligned16(v_out)) return TGVKV_E_INVAL;
-    if ((int64_t)s.B * s.L * s.Hkv * 16 > kMaxBlocks) return TGVKV_E_UNSUPPORTED;
+    if (!units_fit(s, 64)) return TGVKV_E_UNSUPPORTED;
     return hip_status(tgvkv::launch_read_pages(s, pg, first_or_null, count, seg_offsets, out_rows,
                                                static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), stream));
 }
@@ -586,7 +596,7 @@ tgvkv_status tgvkv_chunk_attn_pages(const tgvkv_problem* problem, const tgvkv_op
     st = make_pages(pages, max_pages, block_table, &pg);
     if (st != TGVKV_OK) return st;
     if (decode_reserve < 0 || chunk < 1) return TGVKV_E_INVAL;
-    if (!chunk_fits(s, chunk)) return TGVKV_E_UNSUPPORTED;
+    if (!chunk_fits(s, chunk) || tgvkv::chunk_workgroups(s, chunk) > kMaxWorkgroups) return TGVKV_E_UNSUPPORTED;
     if (s.B == 0) return TGVKV_OK;
     if (!pages_present(pg) || budgets == nullptr || steps == nullptr || q == nullptr || k_new == nullptr ||
         v_new == nullptr || out == nullptr)

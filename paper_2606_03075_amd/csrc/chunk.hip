@@ -1033,6 +1033,12 @@ Plan plan_chunk(const Shape& s, int32_t chunk) {
     return p;
 }
 
+// Workgroups of few_kernel, or of rows_kernel with the units' row tiles in groups of 8 units.
+long long attention_workgroups(const Shape& s, const Plan& p) {
+    const long long units = (long long)s.B * s.L * s.Hkv;
+    return p.extras + (p.few ? units : (units + 7) / 8 * 8 * p.tiles);
+}
+
 size_t partial_floats(const Shape& s, const Plan& p) { return (size_t)2 * p.extras * p.part_rows * (s.D + 2); }
 
 // A number that no other call of the process has; never 0.
@@ -1047,8 +1053,8 @@ unsigned long long call_number() {
 template <int D, int KIND, int PARTS>
 hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st) {
     const Plan p = plan_chunk(s, ck.chunk);
-    const long long units = (long long)s.B * s.L * s.Hkv;
     const size_t lds = lds_pages_bytes(pg);
+    const dim3 grid((unsigned)attention_workgroups(s, p));
     Shares sh{nullptr, nullptr, 0, p.extras};
     if (p.extras > 0) {
         sh.call = call_number();
@@ -1056,7 +1062,6 @@ hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipS
         sh.marks = reinterpret_cast<unsigned long long*>(ck.ws + partial_floats(s, p));
     }
     if (p.few) {
-        const dim3 grid((unsigned)(p.extras + units));
         if (p.nt == 1) hipLaunchKernelGGL((few_kernel<D, KIND, 1, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh);
         else hipLaunchKernelGGL((few_kernel<D, KIND, 2, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh);
         return hipGetLastError();
@@ -1068,7 +1073,6 @@ hipError_t launch_chunk_d(const Shape& s, const Pages& pg, const Chunk& ck, hipS
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)(p.extras + (units + 7) / 8 * 8 * p.tiles));
     if (p.nt == 1)
         hipLaunchKernelGGL((rows_kernel<D, KIND, 1, PARTS>), grid, dim3(kThreads), lds, st, s, pg, ck, sh, p.tiles);
     else
@@ -1084,6 +1088,8 @@ hipError_t launch_chunk_k(const Shape& s, const Pages& pg, const Chunk& ck, hipS
 }
 
 }  // namespace
+
+int64_t chunk_workgroups(const Shape& s, int32_t chunk) { return attention_workgroups(s, plan_chunk(s, chunk)); }
 
 size_t chunk_workspace(const Shape& s, int32_t chunk) {
     const Plan p = plan_chunk(s, chunk);

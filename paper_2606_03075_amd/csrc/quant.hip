@@ -190,10 +190,11 @@ hipError_t launch_read_pages(const Shape& s, const Pages& pg, const int32_t* fir
         hipLaunchKernelGGL(kernel, grid, dim3(threads), lds_pages_bytes(pg), st, s, pg, first, count, seg_off, out_rows,
                            nsplit, kc, vc);
     };
-    // segments of a few rows (what a step or a chunk appended) are work for one wave: 4096 of one row take 4.8 us, in four waves each 7.2
+    // segments of a few rows (what a step or a chunk appended) are work for one wave: 4096 of one row take 4.8 us, in four
+    // waves each 7.2; 2^24 workgroups of four waves are more threads than a launch numbers
     auto pick = [&](auto d, auto kind) {
         constexpr int D = decltype(d)::value, KIND = decltype(kind)::value;
-        if (out_rows <= (int64_t)s.B * s.L * (8 * 64 / D)) launch(read_pages_kernel<D, KIND, 64>, 64);
+        if (out_rows <= (int64_t)s.B * s.L * (8 * 64 / D) || grid.x >= 1u << 24) launch(read_pages_kernel<D, KIND, 64>, 64);
         else launch(read_pages_kernel<D, KIND, kThreads>, kThreads);
     };
     auto pick_kind = [&](auto d) {

@@ -131,6 +131,7 @@ struct Chunk {
     float* ws;
 };
 
+int64_t chunk_workgroups(const Shape& s, int32_t chunk);      // of the larger launch of a call with this chunk
 size_t chunk_workspace(const Shape& s, int32_t chunk);        // bytes that a call with this chunk needs
 size_t chunk_workspace_up_to(const Shape& s, int32_t chunk);  // that any call with at most this chunk does
 hipError_t launch_chunk(const Shape& s, const Pages& pg, const Chunk& ck, hipStream_t st);

@@ -122,6 +122,31 @@ def test_a_store_takes_a_table_of_any_width(so):
     assert store(problem=P(batch=0), pool=pages(k=None)) == 0
 
 
+@pytest.mark.skipif(_gpu(), reason="fake pointers are used only where no GPU exists")
+def test_more_workgroups_than_a_launch_numbers(so):
+    """A launch's threads are numbered in 32 bits; one of 2^24 workgroups of 256 runs only a part of them, without an error
+    (33000 x 512 segments: the last sequence's results were left as they were).  Such calls are refused."""
+    def calls(batch, layers, hq, hkv, chunk=1):
+        p = ctypes.byref(P(batch=batch, layers=layers, heads_q=hq, heads_kv=hkv, head_dim=64, n_sys=0, n_vis=4, n_qst=0))
+        yield "chunk", so.tgvkv_chunk_attn_pages(p, None, pages(), FAKE, 1, FAKE, 4, FAKE, None, chunk, FAKE, FAKE, FAKE, FAKE, 0,
+                                                 FAKE, BIG, None, S)
+        if chunk == 1:
+            for kind in (0, 1):
+                for call in (so.tgvkv_compact_pages, so.tgvkv_store_pages):
+                    yield "store", call(p, None, FAKE, FAKE, FAKE, FAKE, FAKE, layers, pages(kind=kind, size=1024), FAKE, 1, None, S)
+            yield "store", so.tgvkv_store_pages(p, None, FAKE, FAKE, FAKE, FAKE, FAKE, layers, pages(kind=0, size=1), FAKE, 1, None, S)
+            yield "compact", so.tgvkv_compact(p, None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, layers, 1, FAKE, FAKE, None, S)
+            yield "decode", so.tgvkv_decode_attn(p, None, FAKE, FAKE, FAKE, FAKE, 4, 0, FAKE, FAKE, FAKE, FAKE, FAKE, BIG, None, S)
+            yield "decode", so.tgvkv_decode_attn_paged(p, None, FAKE, FAKE, 64, 8, FAKE, 1, FAKE, 4, FAKE, FAKE, FAKE, FAKE, FAKE,
+                                                       FAKE, BIG, None, S)
+    read = lambda batch, layers, hkv: so.tgvkv_read_pages(ctypes.byref(P(  # noqa: E731
+        batch=batch, layers=layers, heads_q=hkv, heads_kv=hkv, head_dim=64)), None, pages(), FAKE, 1, None, FAKE, FAKE, 9, FAKE, FAKE, S)
+    for shape in [(1 << 15, 512, 1, 1), (33000, 512, 2, 1), (1 << 14, 512, 2, 2), (1 << 12, 512, 8, 8), (1 << 13, 512, 2, 2, 130)]:
+        for name, status in calls(*shape):
+            assert status == -2, (name, shape)
+    assert read(1 << 17, 512, 1) == read(1 << 15, 512, 4) == -2  # reads take one wave per segment there
+
+
 def test_stores_check_their_tensors_sizes(so, monkeypatch):
     """A tensor too small for the problem is refused before the call, which reads by the problem's sizes: a short `budgets`
     or `idx` would be read out of range on the GPU.  (Host tensors, taken for the GPU's; the library's calls only count.)"""

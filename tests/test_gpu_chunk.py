@@ -441,6 +441,33 @@ def test_a_loop_keeps_one_workspace(lib, kind):
         check(case(50 + chunk, B, L, hq, hkv, d, chunk, kind, 16, budgets, np.arange(B) % 3, n_new, chunk + 4), ws=ws)
 
 
+def test_the_most_segments(lib):
+    """One less sequence than would make 2^24 workgroups: the first and the last are served, idle ones are left alone; a read
+    of twice as many segments, by one wave each."""
+    import torch
+    log("chunk the most segments")
+    B, L, d = (1 << 15) - 1, 512, 64
+    p, n = bd.make_problem(B, L, 1, 1, d, 1, 0, 0), B * L
+    full = lambda v, *s, t=torch.int32: torch.full(s, v, dtype=t, device="cuda")  # noqa: E731
+    pool = bd.PagedPool(1, d, 8, 4)
+    table, steps = full(0, n, 1), full(-1, B)
+    steps[0], steps[-1], table[:L], table[-L:] = 0, 0, 2, 3
+    new, out = full(1.0, B, L, 1, 1, d, t=torch.bfloat16), full(7.0, B, L, 1, 1, d, t=torch.float32)
+    ws = full(0, max(16, bd.chunk_workspace_size(p, None, 1)), t=torch.uint8)
+    pool.extend(p, None, table, full(0, n), 4, steps, None, new, new, new, out, ws)
+    torch.cuda.synchronize()
+    assert torch.all(out[0] == 1) and torch.all(out[-1] == 1) and torch.all(out[1:-1] == 7)
+    del new, out
+    p, m = bd.make_problem(B, L, 2, 2, d, 1, 0, 0), 2 * n
+    pool = bd.PagedPool(2, d, 8, 4)
+    pool.k_pool.fill_(3.0)
+    pool.v_pool.fill_(-3.0)
+    k, v = full(0.0, m * d, t=torch.bfloat16), full(0.0, m * d, t=torch.bfloat16)
+    pool.read(p, None, table, full(1, n), torch.arange(n + 1, dtype=torch.int64, device="cuda"), k, v)
+    torch.cuda.synchronize()
+    assert torch.all(k == 3) and torch.all(v == -3)
+
+
 def test_other_streams(lib):
     """Two calls at once, each on a stream of its own with a workspace of its own, and the stream argument."""
     import torch
