@@ -309,6 +309,77 @@ def test_a_serving_loop(lib, kind, heads):
             assert np.abs(out[0, l, h].double().cpu().numpy() - want).max() <= 1e-4 * np.abs(v).max()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_captured_admission(lib, kind):
+    """Store, a chunk and a read in one graph, on a stream of its own, replayed with other keys, values, budgets and steps:
+    the same bits as the calls made one by one on another pool, which run between the replays."""
+    import torch
+    log(f"captured admission kind={kind}")
+    B, L, hq, hkv, d, N, page, chunk, reserve, kept = 2, 2, 4, 2, 64, 200, 16, 3, 8, 90
+    p, width = bd.make_problem(B, L, hq, hkv, d, 0, N, 0), -(-(80 + reserve) // page)
+    pools = [bd.PagedPool(hkv, d, page, B * L * width, kind=kind) for _ in range(2)]
+    for pool in pools:  # unwritten pages alike
+        for t in (pool.k_pool, pool.v_pool, pool.k_exp, pool.v_exp):
+            if t is not None:
+                t.view(torch.uint8).zero_()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    zeros = lambda dtype, *s: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    table = torch.randperm(B * L * width, generator=gen, device="cuda").to(torch.int32).view(B * L, width)
+    k, v = rand(B, L, hkv, N, d), rand(B, L, hkv, N, d)
+    q, kn, vn = rand(B, L, chunk, hq, d), rand(B, L, chunk, hkv, d), rand(B, L, chunk, hkv, d)
+    idx, budgets, steps, n_new = zeros(torch.int32, B * kept), zeros(torch.int32, B, L), zeros(torch.int32, B), zeros(torch.int32, B)
+    ioff, seg, count = zeros(torch.int64, B * L + 1), zeros(torch.int64, B * L + 1), zeros(torch.int32, B * L)
+    outs = [(zeros(torch.float32, B, L, chunk, hq, d), rand(B * (kept + L * reserve) * hkv * d), rand(B * (kept + L * reserve) * hkv * d))
+            for _ in range(2)]
+    ws = [torch.empty(max(16, bd.chunk_workspace_size(p, None, chunk)), dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def go(i):
+        out, kc, vc = outs[i]
+        pools[i].store(p, None, k, v, idx, budgets, ioff, kept, table)
+        pools[i].extend(p, None, table, budgets, reserve, steps, n_new, q, kn, vn, out, ws[i])
+        pools[i].read(p, None, table, count, seg, kc, vc)
+    rng = np.random.default_rng(5)
+
+    def change(rep):
+        first = rng.integers(10, 81, B)
+        bud = np.stack([first, kept - first], 1).astype(np.int32)
+        st, n = rng.integers(0, reserve - chunk + 1, B), rng.integers(0, chunk + 1, B)
+        budgets.copy_(_up(bud))
+        steps.copy_(_up(st.astype(np.int32)))
+        n_new.copy_(_up(n.astype(np.int32)))
+        idx.copy_(_up(np.concatenate([np.sort(rng.choice(N, m, replace=False)) for m in bud.reshape(-1)]).astype(np.int32)))
+        ioff.copy_(_up(np.concatenate([[0], np.cumsum(bud.reshape(-1))]).astype(np.int64)))
+        seg.copy_(_up(np.concatenate([[0], np.cumsum(bud.reshape(-1) + reserve)]).astype(np.int64)))
+        count.copy_(_up((bud + (st + n)[:, None]).reshape(-1).astype(np.int32)))
+        for x in (k, v, q, kn, vn):
+            x.copy_(rand(*x.shape))
+        for x, y in zip(*outs):
+            x.fill_(rep)
+            y.fill_(rep)
+    change(0)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        go(0)
+    go(1)  # the rows between the budgets and the steps, which this test does not write, are of earlier calls: the same in both
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        go(0)
+    for rep in range(5):
+        change(rep)
+        torch.cuda.synchronize()
+        graph.replay()
+        go(1)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.int8), y.view(torch.int8)) for x, y in zip(*outs)), rep
+        for name in ("k_pool", "v_pool", "k_exp", "v_exp"):
+            x, y = (getattr(pool, name) for pool in pools)
+            assert x is None or torch.equal(x.view(torch.int8), y.view(torch.int8)), (rep, name)
+
+
 def test_pool_arguments_are_checked(lib):
     import torch
     log("pool checks")
