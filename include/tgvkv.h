@@ -391,7 +391,8 @@ enum { TGVKV_CACHE_BF16 = 0, TGVKV_CACHE_FP8 = 1, TGVKV_CACHE_INT8 = 2 };
 typedef struct tgvkv_pages {
     void*    k;          /* [n_pages][heads_kv][page_size][head_dim], bf16 or codes               */
     void*    v;
-    uint8_t* k_exp;      /* [n_pages][heads_kv][page_size] exponent bytes; unused with BF16        */
+    uint8_t* k_exp;      /* [n_pages][heads_kv][page_size] exponent bytes, 16-byte aligned as the
+                            other tensors; unused with BF16                                        */
     uint8_t* v_exp;
     int64_t  n_pages;    /* 1 .. 2^31 - 1                                                          */
     int32_t  page_size;  /* a power of two in [1, 4096]                                            */
@@ -448,7 +449,8 @@ tgvkv_status tgvkv_read_pages(const tgvkv_problem* problem, const tgvkv_opts* op
  * q            bf16 [B][L][chunk][heads_q][head_dim];  k_new, v_new bf16 [B][L][chunk][heads_kv][head_dim]
  * steps, n_new_or_null  int32 [B], device
  * out          [B][L][chunk][heads_q][head_dim], f32, or bf16 with out_bf16 != 0 (the probabilities then enter
- *              the product with the values in bf16 too, not in three bf16 parts)
+ *              the product with the values in bf16 too, not in three bf16 parts: two roundings; f32 results
+ *              rounded by the caller have one)
  * Limits: chunk >= 1 (TGVKV_E_INVAL); B * L * chunk * heads_q <= 2^31 - 1, and fewer than 2^24 workgroups, one per
  * segment and KV head and, above 32 query rows chunk * heads_q / heads_kv, per 64 or (above 64) 128 of these
  * (TGVKV_E_UNSUPPORTED).

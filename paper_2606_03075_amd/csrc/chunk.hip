@@ -12,7 +12,8 @@
 //                 softmax, so a new maximum rescales a lane's values by the lane's own factor.
 // With 32-bit results the probabilities enter as three bf16 parts, all of their 24 bits (errors of 2e-7 against 64 bits;
 // two parts left 2e-6, and three take 0 to 2 % longer where the cache is read, 8 % where products bound the
-// call); with bf16 results as one, off by 2^-8 at most like the result itself.
+// call); with bf16 results as one, off by 2^-8 at most like the result itself (2.3e-3 against 64 bits, where a result in
+// 32 bits rounded once has 1.7e-3; a caller who wants that takes 32-bit results and rounds them).
 //
 // An 8-bit code times its row's power of two is a bf16, so the products take bf16 whatever the pages hold.
 //
@@ -21,10 +22,11 @@
 //                rows and takes every fourth block of 32 keys, staged in LDS of its own, no barrier; codes stay codes
 //                in LDS (half of it: three workgroups per CU instead of two).  The new rows are one more block,
 //                quantised and written to the pages on the way.  4096 units of 215 rows of e4m3, one query row each:
-//                56 us, 4.2 TB/s; the loads alone take 43.  Bound by instruction issue (76 % busy) and the units' set-up.
+//                57 us, 4.1 TB/s; the loads alone take 43.  Bound by instruction issue (78 % busy) and the units' set-up.
 //   rows_kernel  more: a wave holds 16 NT rows of its own, and 64 keys at a time are staged as bf16 for the workgroup.
-//                1000 tokens of 4 sequences, 28 layers, 28/4 heads of 128, bf16 results: 2.1 ms, 740 TFLOP/s.  Bound by
-//                what two waves per SIMD overlap of LDS waits, exponentials and products.
+//                1000 tokens of 4 sequences, 28 layers, 28/4 heads of 128, bf16 results: 2.10 ms, 750 TFLOP/s, in a steady
+//                run (in a short one from a cold start 2.1 to 2.25).  Bound by what two waves per SIMD overlap of LDS
+//                waits, exponentials and products.
 //
 // A value that is not finite in a new token's V would reach earlier tokens through 0 * inf; such elements
 // are staged as 0 and added to the rows that see them at the end (rare: one flag is looked at), after the last
@@ -889,10 +891,11 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
                 }
             }
         }
-        // Where the call is a read of the retained rows, once (one row tile per unit, few tokens), they are streamed: 5 tokens
-        // on the video shape 67 us against 75.  Several tiles find the keys in L2, and with more tokens, whose
-        // rows are read again to be written to the pages, plain loads are faster: 64 tokens of the LLaVA-NeXT shape
-        // 185 us against 199.
+        // Where the call is a read of the retained rows, once (one row tile per unit, few tokens), they are streamed: 5 tokens of
+        // 7 heads on the video shape 67 us against 75.  Several tiles find the keys in L2, and with more tokens, whose
+        // rows are read again to be written to the pages, plain loads are faster: 64 tokens of one head on the LLaVA-NeXT shape
+        // 185 us against 199.  Only these two were measured.  With 33 to 64 query rows (NT = 1) the limit lies between them:
+        // up to 31 tokens means two heads or more per KV head, 33 and more means one.
         if (NT == 1 && ck.chunk < kStreamChunk) {
             asm volatile("; streamed");  // the compiler would merge the two branches' loads, and drop the hint
 #pragma unroll
@@ -1010,7 +1013,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void rows_kernel(Shape s
 // Workgroups for further shares, in calls of up to so many items.  Few extras make long shares, and each costs its
 // scan whether there is a share for it or not: five tokens on the video shape (896 items, layers of 139 to 5449 rows)
 // 82 us with 256, 62 with 384, 60 with 448, 67 with 512, 76 with 1024; single tokens there on 8-bit pages 67, 54, 54,
-// 54 and 62 us.  More items than that even out by themselves, longest first.
+// 54 and 62 us.  The number was chosen on this one shape, whatever a call's items.  More items than kItemsOfExtras even
+// out in part, longest first: a step from 2016 to 2128 items of such layers (18 and 19 sequences) takes five tokens
+// from 110 to 167 us, single tokens on bf16 pages from 90 to 93 and on int8 pages from 63 to 78; without unit_order,
+// 161 to 251, 105 to 143 and 83 to 125.
 constexpr int kExtras = 448, kItemsOfExtras = 2048;
 
 // How a call is dealt out.
