@@ -447,9 +447,10 @@ def chunk_workspace_size(problem, opts, chunk) -> int:
 
 def _room(t, kind, n, device, name):
     """_at of a tensor of at least n elements (or no tensor)."""
-    if t is not None and isinstance(t, _torch.Tensor) and t.numel() < n:
+    at = _at(t, kind, None, device, name)
+    if t is not None and t.numel() < n:
         raise ValueError(f"{name} must hold {n} elements")
-    return _at(t, kind, None, device, name)
+    return at
 
 
 def _store(fn, problem, opts, k, v, idx, budgets, idx_offsets, total_budget, pool, block_table, stream, unit_order):
