@@ -13,7 +13,8 @@
 // With 32-bit results the probabilities enter as three bf16 parts, all of their 24 bits (errors of 2e-7 against 64 bits;
 // two parts left 2e-6, and three take 0 to 2 % longer where the cache is read, 8 % where products bound the
 // call); with bf16 results as one, off by 2^-8 at most like the result itself (2.3e-3 against 64 bits, where a result in
-// 32 bits rounded once has 1.7e-3; a caller who wants that takes 32-bit results and rounds them).
+// 32 bits rounded once has 1.7e-3, as two parts have: 2.66 ms for 2.10 with 1000 tokens of the video shape, 169 us for 141
+// with 48 on e4m3 pages.  A caller who wants the one rounding takes 32-bit results and rounds them).
 //
 // An 8-bit code times its row's power of two is a bf16, so the products take bf16 whatever the pages hold.
 //
